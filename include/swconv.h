@@ -340,6 +340,118 @@ int swconv_plan_sizes(const swconv_plan* plan, int* P, int64_t* T, int* Ho, int*
 int swconv_plan_weight_stats(const swconv_plan* plan, int64_t* nnz, int64_t* padded_nnz, int* work_items,
                              int64_t* max_item);
 
+/*
+ * Element types of the activations and scores below; sums, parameters and statistics are fp32 with all of them.
+ */
+typedef enum {
+  SWCONV_F32 = 0,
+  SWCONV_F16 = 1, /* IEEE half precision */
+  SWCONV_BF16 = 2
+} swconv_dtype;
+
+/*
+ * Bias, ReLU and dropout in one pass, between two layers of a network in training (or, with p = 0, at inference):
+ *     z = x + bias[k],   a = relu ? max(z, 0) : z,   y = a / (1 - p) with probability 1 - p, else 0
+ * enqueued on `hip_stream` as one kernel; nothing is allocated, no mask is stored.
+ *   dtype       a swconv_dtype, of x and y
+ *   N, K, S     x is N x K x S: feature maps of S = Ho*Wo pixels (the layer's output), or with S = 1 N rows of K
+ *               features (tokens or images in front of a classifier).  N = 0 is legal and does nothing.
+ *   x_dev       DEVICE, image n at x_dev + n*x_stride elements, its K x S values contiguous; any alignment of an
+ *               element.  x_stride >= K*S as in swconv_plan_set_image_strides; 0 means K*S.
+ *   bias_dev    DEVICE, K floats, or NULL
+ *   p           the dropout rate, 0 <= p <= 1, rounded to a multiple of 2^-16 (the scale is that of the rounded
+ *               rate).  0: nothing is dropped and rng_dev is not read; 1: y = 0.
+ *   rng_dev     DEVICE, two 64-bit words: the seed and a step count, read when the kernel runs - a captured graph
+ *               makes new masks when the caller's program changes them between replays.
+ *   offset      added to the step count (mod 2^64), e.g. the number of the layer.  Calls of equal seed and step + offset
+ *               and equal shape make equal masks.
+ *   y_dev       DEVICE, N x K x S with y_stride; may be x_dev with the same stride, else shares no element with x.
+ *               Elements between the images are neither read nor written.
+ * The mask is a function of the sizes and the four numbers alone, whatever dtype, strides and launch: with
+ * row = n*K + k, col = s (S = 1: row = n, col = k) an element is kept if the 16-bit field col % 8 (low half of word 0
+ * first) of philox4x32-10 at counter {col / 8, row, low and high word of step + offset} with the seed as key is not
+ * below p * 2^16.  Dropped elements are 0 whatever x holds (NaN included); arithmetic is fp32, rounded once.
+ * Errors: EINVAL (unknown dtype, negative or zero sizes, a stride below K*S, null or misaligned pointers, p out of
+ * range or NaN, tensors that overlap in another way), EUNSUPPORTED (N, K or S >= 2^31, N*K >= 2^32 maps, more than
+ * 2^40 elements from the first to the last), EHIP.
+ */
+int swconv_dropout_forward(int dtype, int64_t N, int64_t K, int64_t S, const void* x_dev, int64_t x_stride,
+                           const float* bias_dev, int relu, float p, const uint64_t* rng_dev, uint64_t offset,
+                           void* hip_stream, void* y_dev, int64_t y_stride);
+
+/*
+ * The backward pass of swconv_dropout_forward, which makes the same mask again from the same sizes, p, rng_dev
+ * contents and offset:
+ *     dz = dy / (1 - p) where kept (and, with relu, unless z <= 0), else 0;   dx = dz,   dbias[k] = sum over n, s of dz
+ *   dy_dev         DEVICE, N x K x S with dy_stride
+ *   x_dev          DEVICE, the forward pass's input, with its bias_dev; read with relu only (else both may be NULL)
+ *   workspace_dev  DEVICE, 4-byte aligned, swconv_dropout_workspace_bytes(N, K, S) bytes; used with dbias_dev only, may be
+ *                  NULL where that is 0.  Its contents do not matter; calls that overlap in time need one each.
+ *   dx_dev         DEVICE, N x K x S with dx_stride, or NULL; may be dy_dev or x_dev with the same stride
+ *   dbias_dev      DEVICE, K floats, or NULL; overwritten (with 0 for N = 0).  Summed in fp32 from dz before its
+ *                  rounding to dtype, in an order that depends on the sizes only: equal calls give equal bits.
+ * One kernel, with dbias_dev a second small one.  Errors as for swconv_dropout_forward; EINVAL for a workspace that is too
+ * small and for neither dx_dev nor dbias_dev.
+ */
+int swconv_dropout_backward(int dtype, int64_t N, int64_t K, int64_t S, const void* dy_dev, int64_t dy_stride,
+                            const void* x_dev, int64_t x_stride, const float* bias_dev, int relu, float p,
+                            const uint64_t* rng_dev, uint64_t offset, void* workspace_dev, int64_t workspace_bytes,
+                            void* hip_stream, void* dx_dev, int64_t dx_stride, float* dbias_dev);
+
+/* Bytes of workspace that swconv_dropout_backward needs for dbias_dev; touches no device.  Errors as there. */
+int swconv_dropout_workspace_bytes(int64_t N, int64_t K, int64_t S, int64_t* bytes);
+
+/*
+ * Log probabilities at a network's end: for every row of scores (the classes of an image, the vocabulary of a token)
+ *     m = max_j x_j,   ls = log sum_j exp(x_j - m),   log p_j = (x_j - m) - ls
+ * the log probability of the given class, the entropy and the best classes, in one pass over the scores; enqueued on
+ * `hip_stream` (one kernel, two for few long rows); nothing is allocated.
+ *   dtype            a swconv_dtype, of the scores
+ *   rows, classes    rows = 0 is legal and does nothing; 1 <= classes < 2^31 - 4096
+ *   scores_dev       DEVICE, row i at scores_dev + i*row_stride elements (0: classes); any alignment of an element;
+ *                    what lies between the rows is not read
+ *   labels_dev       DEVICE, rows int32: the class asked for; below 0: none in this row.  May be NULL without
+ *                    logprob_dev.
+ *   top              how many of the best classes, 0 <= top <= 64 (it may exceed `classes`)
+ *   workspace_dev    DEVICE, 16-byte aligned, swconv_logprobs_workspace_bytes(dtype, rows, classes, top) bytes, may be NULL
+ *                    where that is 0.  Its contents do not matter; calls that overlap in time need one each.
+ *   logprob_dev      DEVICE, rows floats or NULL: log p of the label, 0 where there is none
+ *   entropy_dev      DEVICE, rows floats or NULL: -sum_j p_j log p_j
+ *   stats_dev        DEVICE, rows x 2 floats or NULL: m and ls, for swconv_logprobs_backward
+ *   top_class_dev, top_logprob_dev   DEVICE, rows x top int32 and floats, both or (top = 0) neither: the classes of the
+ *                    largest scores in descending order, of equal scores (0 and -0 too) the lower class first
+ * Sums are fp32.  A score of -inf is masked: it has probability 0 and is never among the best; places that no class is left
+ * for hold -1 and -inf.  A row without any unmasked class has m = -inf, ls = 0, log p = -inf and entropy 0.  The types'
+ * lowest finite values are scores like others.  A row that holds NaN or +inf gives NaN for every float and -1
+ * for every class; a label >= classes gives NaN (and reads nothing).
+ * Errors: EINVAL (unknown dtype, rows < 0, classes < 1, top < 0, a stride below `classes`, null or misaligned pointers,
+ * no output, a workspace that is too small), EUNSUPPORTED (sizes beyond these, top > 64), EHIP.
+ */
+int swconv_logprobs_forward(int dtype, int64_t rows, int64_t classes, const void* scores_dev, int64_t row_stride,
+                            const int32_t* labels_dev, int top, void* workspace_dev, int64_t workspace_bytes,
+                            void* hip_stream, float* logprob_dev, float* entropy_dev, float* stats_dev,
+                            int32_t* top_class_dev, float* top_logprob_dev);
+
+/* Bytes of workspace that swconv_logprobs_forward needs; touches no device.  Errors as there. */
+int swconv_logprobs_workspace_bytes(int dtype, int64_t rows, int64_t classes, int top, int64_t* bytes);
+
+/*
+ * The gradient of a loss over what swconv_logprobs_forward gave, with g = dL/d(logprob) and h = dL/d(entropy) of a row:
+ *     dL/dx_j = g ([j = label] - p_j) - h p_j (log p_j + H)
+ * (a mean negative log probability over n rows has g = -1/n), enqueued on `hip_stream` as one kernel.
+ *   scores_dev, labels_dev, stats_dev, entropy_dev   as given to and by the forward pass
+ *   dlogprob_dev    DEVICE, rows floats or NULL: g; needs labels_dev.  Not used in rows whose label is below 0.
+ *   dentropy_dev    DEVICE, rows floats or NULL: h; needs entropy_dev.  One of the two at least.
+ *   dscores_dev     DEVICE, rows x classes with dscores_stride (0: classes), in dtype, rounded once; may be scores_dev with
+ *                   the same stride.  What lies between the rows is not written.
+ * Masked classes (score -inf) get 0, the label's too; rows of NaN statistics and of labels >= classes with a
+ * dlogprob_dev get NaN.  Errors as for swconv_logprobs_forward.
+ */
+int swconv_logprobs_backward(int dtype, int64_t rows, int64_t classes, const void* scores_dev, int64_t row_stride,
+                             const int32_t* labels_dev, const float* stats_dev, const float* entropy_dev,
+                             const float* dlogprob_dev, const float* dentropy_dev, void* hip_stream, void* dscores_dev,
+                             int64_t dscores_stride);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,6 +11,7 @@ import numpy as np
 from . import build as _build
 
 SWCONV_OK, SWCONV_EINVAL, SWCONV_EUNSUPPORTED, SWCONV_ENOMEM, SWCONV_EHIP, SWCONV_ESTATE = range(6)
+SWCONV_F32, SWCONV_F16, SWCONV_BF16 = range(3)
 
 EXPORTS = [
     "swconv_status_string", "swconv_plan_create", "swconv_plan_destroy", "swconv_set_weights",
@@ -20,6 +21,8 @@ EXPORTS = [
     "swconv_backward", "swconv_debug_copy_dZ", "swconv_debug_copy_dV", "swconv_profile_backward",
     "swconv_prune_step", "swconv_set_weights_device", "swconv_plan_set_image_strides",
     "swconv_update_values", "swconv_forward_noalloc",
+    "swconv_dropout_forward", "swconv_dropout_backward", "swconv_dropout_workspace_bytes",
+    "swconv_logprobs_forward", "swconv_logprobs_backward", "swconv_logprobs_workspace_bytes",
 ]
 
 _lib = None
@@ -68,6 +71,14 @@ def lib():
         L.swconv_set_weights_device.argtypes = [_vp] * 5
         L.swconv_debug_copy_dZ.argtypes = [_vp, _f32p]
         L.swconv_debug_copy_dV.argtypes = [_vp, _f32p]
+        i, i64, u64 = ctypes.c_int, ctypes.c_int64, ctypes.c_uint64
+        L.swconv_dropout_forward.argtypes = [i, i64, i64, i64, _vp, i64, _vp, i, ctypes.c_float, _vp, u64, _vp, _vp, i64]
+        L.swconv_dropout_backward.argtypes = [i, i64, i64, i64, _vp, i64, _vp, i64, _vp, i, ctypes.c_float, _vp, u64, _vp,
+                                              i64, _vp, _vp, i64, _vp]
+        L.swconv_dropout_workspace_bytes.argtypes = [i64, i64, i64, ctypes.POINTER(i64)]
+        L.swconv_logprobs_forward.argtypes = [i, i64, i64, _vp, i64, _vp, i, _vp, i64] + [_vp] * 6
+        L.swconv_logprobs_backward.argtypes = [i, i64, i64, _vp, i64] + [_vp] * 7 + [i64]
+        L.swconv_logprobs_workspace_bytes.argtypes = [i, i64, i64, i, ctypes.POINTER(i64)]
         _lib = L
     return _lib
 
@@ -190,6 +201,49 @@ def swconv_profile_forward(plan, stream, in_dev_ptr, out_dev_ptr, iters):
 
 def swconv_update_values(plan, stream, vals_dev_ptr):
     _check(lib().swconv_update_values(plan, _vp(stream), _vp(vals_dev_ptr)), "swconv_update_values")
+
+
+def swconv_dropout_forward(dtype, N, K, S, x_dev, x_stride, bias_dev, relu, p, rng_dev, offset, stream, y_dev, y_stride):
+    """dtype: SWCONV_F32, SWCONV_F16 or SWCONV_BF16; device addresses as int (0: none), strides in elements (0: dense)."""
+    _check(lib().swconv_dropout_forward(dtype, N, K, S, x_dev, x_stride, bias_dev, relu, p, rng_dev, offset, stream, y_dev,
+                                        y_stride), "swconv_dropout_forward")
+
+
+def swconv_dropout_backward(dtype, N, K, S, dy_dev, dy_stride, x_dev, x_stride, bias_dev, relu, p, rng_dev, offset,
+                            workspace_dev, workspace_bytes, stream, dx_dev, dx_stride, dbias_dev):
+    """Device addresses as int; x_dev and bias_dev are read with relu only, dx_dev or dbias_dev may be 0 (not wanted)."""
+    _check(lib().swconv_dropout_backward(dtype, N, K, S, dy_dev, dy_stride, x_dev, x_stride, bias_dev, relu, p, rng_dev,
+                                         offset, workspace_dev, workspace_bytes, stream, dx_dev, dx_stride, dbias_dev),
+           "swconv_dropout_backward")
+
+
+def swconv_dropout_workspace_bytes(N, K, S):
+    n = ctypes.c_int64()
+    _check(lib().swconv_dropout_workspace_bytes(N, K, S, ctypes.byref(n)), "swconv_dropout_workspace_bytes")
+    return n.value
+
+
+def swconv_logprobs_forward(dtype, rows, classes, scores_dev, row_stride, labels_dev, top, workspace_dev, workspace_bytes,
+                            stream, logprob_dev, entropy_dev, stats_dev, top_class_dev, top_logprob_dev):
+    """Device addresses as int; outputs that are not wanted are 0."""
+    _check(lib().swconv_logprobs_forward(dtype, rows, classes, scores_dev, row_stride, labels_dev, top, workspace_dev,
+                                         workspace_bytes, stream, logprob_dev, entropy_dev, stats_dev, top_class_dev,
+                                         top_logprob_dev), "swconv_logprobs_forward")
+
+
+def swconv_logprobs_workspace_bytes(dtype, rows, classes, top):
+    n = ctypes.c_int64()
+    _check(lib().swconv_logprobs_workspace_bytes(dtype, rows, classes, top, ctypes.byref(n)),
+           "swconv_logprobs_workspace_bytes")
+    return n.value
+
+
+def swconv_logprobs_backward(dtype, rows, classes, scores_dev, row_stride, labels_dev, stats_dev, entropy_dev, dlogprob_dev,
+                             dentropy_dev, stream, dscores_dev, dscores_stride):
+    """Device addresses as int; dlogprob_dev or dentropy_dev (with entropy_dev) may be 0."""
+    _check(lib().swconv_logprobs_backward(dtype, rows, classes, scores_dev, row_stride, labels_dev, stats_dev, entropy_dev,
+                                          dlogprob_dev, dentropy_dev, stream, dscores_dev, dscores_stride),
+           "swconv_logprobs_backward")
 
 
 def swconv_plan_set_image_strides(plan, in_stride, out_stride):

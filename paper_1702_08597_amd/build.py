@@ -7,7 +7,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libswconv.so")
-SOURCES = [os.path.join(CSRC, "swconv.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("swconv.hip", "swconv_training.hip")]
 HEADERS = [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith((".hpp", ".inc"))]
 HEADERS.append(os.path.join(os.path.dirname(HERE), "include", "swconv.h"))
 

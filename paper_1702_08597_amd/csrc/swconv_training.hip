@@ -1,0 +1,343 @@
+// Host side of what stands around a layer in training and at a network's end: bias, ReLU and dropout, and log
+// probabilities, each with its gradient.  Independent of any plan; the calls keep nothing, allocate nothing and only
+// enqueue kernels.
+#include "../../include/swconv.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "swconv_dropout_kernels.hpp"
+#include "swconv_logprobs_kernels.hpp"
+
+using namespace swconv;
+
+namespace {
+
+constexpr int64_t kMost = (int64_t)1 << 40;  // elements between a tensor's first and last one
+constexpr int64_t kMaxGroups = (int64_t)1 << 20;  // workgroups of a launch; more work is done in turns
+
+// The stream's device while a call launches, if that is not the current one.
+class StreamDevice {
+ public:
+  explicit StreamDevice(hipStream_t st) {
+    static const int count = [] {
+      int n = 0;
+      if (hipGetDeviceCount(&n) != hipSuccess) (void)hipGetLastError();
+      return n;
+    }();
+    if (count < 2 || !st || st == hipStreamLegacy || st == hipStreamPerThread) return;
+    hipDevice_t dev = 0;
+    int now = 0;
+    if (hipStreamGetDevice(st, &dev) != hipSuccess || hipGetDevice(&now) != hipSuccess) {
+      (void)hipGetLastError();
+      return;
+    }
+    if ((int)dev != now && hipSetDevice((int)dev) == hipSuccess) back_ = now;
+  }
+  ~StreamDevice() {
+    if (back_ >= 0 && hipSetDevice(back_) != hipSuccess) (void)hipGetLastError();
+  }
+  StreamDevice(const StreamDevice&) = delete;
+
+ private:
+  int back_ = -1;
+};
+
+template <typename... Params, typename... Args>
+int launch(void (*kern)(Params...), dim3 grid, int block, hipStream_t st, Args... args) {
+  hipLaunchKernelGGL(kern, grid, dim3(block), 0, st, Params(args)...);
+  return hipGetLastError() == hipSuccess ? SWCONV_OK : SWCONV_EHIP;
+}
+
+bool known_type(int dtype) { return dtype == SWCONV_F32 || dtype == SWCONV_F16 || dtype == SWCONV_BF16; }
+int64_t size_of(int dtype) { return dtype == SWCONV_F32 ? 4 : 2; }
+
+template <typename F>
+int dispatch_type(int dtype, F&& f) {
+  using std::integral_constant;
+  if (dtype == SWCONV_F32) return f(integral_constant<Elem, Elem::f32>{});
+  if (dtype == SWCONV_F16) return f(integral_constant<Elem, Elem::f16>{});
+  return f(integral_constant<Elem, Elem::bf16>{});
+}
+
+// Rows of `span` elements, `stride` apart.
+struct Rows {
+  const void* p;
+  int64_t rows, span, stride;
+};
+bool placed(const Rows& a, int64_t size) { return a.p && (uintptr_t)a.p % size == 0; }
+// An output may be the input itself, or share no element with it (one row may lie between two of the other's).
+bool may_write(const Rows& out, const Rows& in, int64_t size) {
+  if (!in.p || !out.p || (out.p == in.p && out.stride == in.stride)) return true;
+  const int64_t out_len = ((out.rows - 1) * out.stride + out.span) * size, in_len = ((in.rows - 1) * in.stride + in.span) * size;
+  const uintptr_t o = (uintptr_t)out.p, i = (uintptr_t)in.p;
+  if (o + (uintptr_t)out_len <= i || i + (uintptr_t)in_len <= o) return true;
+  if (out.stride != in.stride) return false;
+  const int64_t step = out.stride * size, off = (int64_t)(o - i) % step, at = off < 0 ? off + step : off;
+  return at >= in.span * size && at + out.span * size <= step;
+}
+
+int ceil_log2(int64_t n) {
+  int s = 0;
+  while (((int64_t)1 << s) < n) ++s;
+  return s;
+}
+
+// ---- dropout ------------------------------------------------------------------------------------------------------
+
+// Sizes: the generator counts rows in 32 bits, a tensor spans at most 2^40 elements.
+int check_sizes(int64_t N, int64_t K, int64_t S) {
+  if (N < 0 || K < 1 || S < 1) return SWCONV_EINVAL;
+  if (N >= (int64_t)1 << 31 || K >= (int64_t)1 << 31 || S >= (int64_t)1 << 31) return SWCONV_EUNSUPPORTED;
+  if (S > 1 && N * K >= (int64_t)1 << 32) return SWCONV_EUNSUPPORTED;
+  if (K * S > kMost) return SWCONV_EUNSUPPORTED;
+  return SWCONV_OK;
+}
+int image_stride(int64_t N, int64_t K, int64_t S, int64_t given, int64_t* stride) {
+  *stride = given ? given : K * S;
+  if (*stride < K * S) return SWCONV_EINVAL;
+  return *stride > kMost || (N > 1 && (N - 1) > kMost / *stride) ? SWCONV_EUNSUPPORTED : SWCONV_OK;
+}
+
+DropoutShape shape_of(int64_t N, int64_t K, int64_t S) {
+  const int64_t rows = S == 1 ? N : N * K, cols = S == 1 ? K : S, groups = (cols + 7) / 8;
+  return {Divisor((uint64_t)groups), Divisor32((uint32_t)groups), Divisor32((uint32_t)K), (uint64_t)(rows * groups), (uint32_t)cols, S == 1};
+}
+
+int rule_of(int64_t N, int relu, float p, const uint64_t* rng, uint64_t offset, DropoutRule* rule) {
+  if (!(p >= 0.0f && p <= 1.0f)) return SWCONV_EINVAL;
+  const uint32_t threshold = (uint32_t)std::lrint((double)p * 65536.0);
+  if (N && threshold && (!rng || (uintptr_t)rng % sizeof(uint64_t))) return SWCONV_EINVAL;
+  *rule = {rng, offset, threshold, threshold < 65536 ? 65536.0f / (float)(65536 - threshold) : 0.0f, relu != 0};
+  return SWCONV_OK;
+}
+
+// How the bias gradient is summed: partial sums in `parts` rows of K.
+struct BiasParts {
+  int64_t parts;
+  MapUnits units{0, Divisor32(1), 0, 0, 1, 6};
+  int across_shift = 0;
+  int64_t col_blocks = 1, rows_per_chunk = 1;
+};
+BiasParts bias_parts(int64_t N, int64_t K, int64_t S) {
+  BiasParts b;
+  const int64_t cols = S == 1 ? K : S, groups = (cols + 7) / 8;
+  if (S > 1) {
+    const int64_t segments = (groups + kDropUnit - 1) / kDropUnit;
+    const int planes = (int)std::clamp<int64_t>(kDropUnit / groups, 1, 64);
+    b.units = {(uint64_t)((N * K + planes - 1) / planes * segments), Divisor32((uint32_t)segments), (uint32_t)(N * K), (uint32_t)N, planes,
+               6 - ceil_log2(planes)};
+    b.parts = N * segments;
+  } else {
+    b.across_shift = std::min(8, ceil_log2(groups));
+    const int64_t across = (int64_t)1 << b.across_shift, down = kDropThreads / across;
+    b.col_blocks = (groups + across - 1) / across;
+    // 1024 workgroups, of at least 4 rows a thread
+    const int64_t chunks = std::clamp<int64_t>((N + 4 * down - 1) / (4 * down), 1, std::max<int64_t>(1, 1024 / b.col_blocks));
+    b.rows_per_chunk = (N + chunks - 1) / std::max<int64_t>(chunks, 1);
+    b.parts = b.rows_per_chunk ? (N + b.rows_per_chunk - 1) / b.rows_per_chunk : 0;
+  }
+  return b;
+}
+
+// ---- log probabilities --------------------------------------------------------------------------------------------
+
+int check_scores(int dtype, int64_t rows, int64_t classes, int64_t given, int64_t* stride) {
+  if (!known_type(dtype) || rows < 0 || classes < 1) return SWCONV_EINVAL;
+  if (classes >= ((int64_t)1 << 31) - 4096) return SWCONV_EUNSUPPORTED;  // class numbers of 32 bits, a tile further
+  *stride = given ? given : classes;
+  if (*stride < classes) return SWCONV_EINVAL;
+  return rows > kMost || *stride > kMost || (rows > 1 && rows - 1 > kMost / *stride) ? SWCONV_EUNSUPPORTED : SWCONV_OK;
+}
+
+// One wave takes rows of up to 2048 classes; longer ones a workgroup, and where there are few rows several.
+struct Parts {
+  bool wave;
+  int parts;
+  int64_t part_classes;
+};
+Parts parts_of(int dtype, int64_t rows, int64_t classes) {
+  if (classes <= 2048) return {true, 1, classes};
+  const int64_t tile = 4 * 64 * (16 / size_of(dtype)) * kLogpUnroll;
+  int64_t parts = std::clamp<int64_t>(1024 / std::max<int64_t>(rows, 1), 1, std::max<int64_t>(1, classes / (4 * tile)));
+  parts = std::min<int64_t>(parts, 64);
+  int64_t part = (classes + parts - 1) / parts;
+  part = (part + tile - 1) / tile * tile;
+  return {false, (int)((classes + part - 1) / part), part};
+}
+int64_t parts_bytes(const Parts& p, int64_t rows, int top) {
+  return p.parts == 1 ? 0 : rows * p.parts * ((int64_t)sizeof(PartSums) + top * (int64_t)sizeof(TopKey));
+}
+
+}  // namespace
+
+extern "C" {
+
+int swconv_dropout_forward(int dtype, int64_t N, int64_t K, int64_t S, const void* x_dev, int64_t x_stride, const float* bias_dev, int relu,
+                           float p, const uint64_t* rng_dev, uint64_t offset, void* hip_stream, void* y_dev, int64_t y_stride) {
+  int rc;
+  DropoutRule rule;
+  if (!known_type(dtype)) return SWCONV_EINVAL;
+  if ((rc = check_sizes(N, K, S)) || (rc = image_stride(N, K, S, x_stride, &x_stride)) ||
+      (rc = image_stride(N, K, S, y_stride, &y_stride)) || (rc = rule_of(N, relu, p, rng_dev, offset, &rule)))
+    return rc;
+  if (N == 0) return SWCONV_OK;
+  const int64_t size = size_of(dtype);
+  const Rows x{x_dev, N, K * S, x_stride}, y{y_dev, N, K * S, y_stride};
+  if (!placed(x, size) || !placed(y, size) || !may_write(y, x, size) || (uintptr_t)bias_dev % 4) return SWCONV_EINVAL;
+  const hipStream_t st = (hipStream_t)hip_stream;
+  const StreamDevice device(st);
+  const DropoutShape sh = shape_of(N, K, S);
+  const int64_t turn = kDropThreads * kDropItems;
+  const dim3 grid((unsigned)std::min<int64_t>(((int64_t)sh.items + turn - 1) / turn, kMaxGroups));
+  return dispatch_type(dtype, [&](auto e) {
+    constexpr Elem E = decltype(e)::value;
+    return launch(dropout_kernel<E, false>, grid, kDropThreads, st, sh, rule, (const elem_t<E>*)x_dev, x_stride, bias_dev,
+                  (const elem_t<E>*)nullptr, (int64_t)0, (elem_t<E>*)y_dev, y_stride);
+  });
+}
+
+int swconv_dropout_workspace_bytes(int64_t N, int64_t K, int64_t S, int64_t* bytes) {
+  if (!bytes) return SWCONV_EINVAL;
+  if (int rc = check_sizes(N, K, S)) return rc;
+  const int64_t parts = bias_parts(N, K, S).parts;
+  *bytes = parts > 1 ? parts * K * (int64_t)sizeof(float) : 0;
+  return SWCONV_OK;
+}
+
+int swconv_dropout_backward(int dtype, int64_t N, int64_t K, int64_t S, const void* dy_dev, int64_t dy_stride, const void* x_dev,
+                            int64_t x_stride, const float* bias_dev, int relu, float p, const uint64_t* rng_dev, uint64_t offset,
+                            void* workspace_dev, int64_t workspace_bytes, void* hip_stream, void* dx_dev, int64_t dx_stride,
+                            float* dbias_dev) {
+  int rc;
+  DropoutRule rule;
+  if (!known_type(dtype)) return SWCONV_EINVAL;
+  if ((rc = check_sizes(N, K, S)) || (rc = image_stride(N, K, S, dy_stride, &dy_stride)) ||
+      (rc = image_stride(N, K, S, x_stride, &x_stride)) || (rc = image_stride(N, K, S, dx_stride, &dx_stride)) ||
+      (rc = rule_of(N, relu, p, rng_dev, offset, &rule)))
+    return rc;
+  if ((uintptr_t)bias_dev % 4 || (uintptr_t)dbias_dev % 4 || (uintptr_t)workspace_dev % 4) return SWCONV_EINVAL;
+  const hipStream_t st = (hipStream_t)hip_stream;
+  const BiasParts bp = bias_parts(N, K, S);
+  const dim3 sum_grid((unsigned)((K + kBiasCols - 1) / kBiasCols));
+  if (N == 0) {
+    if (!dbias_dev) return SWCONV_OK;
+    const StreamDevice device(st);
+    return launch(bias_grad_kernel, sum_grid, kBiasCols * kBiasDown, st, (const float*)nullptr, 0u, (uint32_t)K, dbias_dev);
+  }
+  const int64_t size = size_of(dtype);
+  const Rows dy{dy_dev, N, K * S, dy_stride}, x{relu ? x_dev : nullptr, N, K * S, x_stride}, dx{dx_dev, N, K * S, dx_stride};
+  if (!placed(dy, size) || (relu && !placed(x, size)) || (!dx_dev && !dbias_dev)) return SWCONV_EINVAL;
+  if (dx_dev && (!placed(dx, size) || !may_write(dx, dy, size) || !may_write(dx, x, size))) return SWCONV_EINVAL;
+  const DropoutShape sh = shape_of(N, K, S);
+  if (dbias_dev && bp.parts > 1 && (!workspace_dev || workspace_bytes < bp.parts * K * (int64_t)sizeof(float))) return SWCONV_EINVAL;
+  float* partial = bp.parts > 1 ? (float*)workspace_dev : dbias_dev;
+  const StreamDevice device(st);
+  rc = dispatch_type(dtype, [&](auto e) {
+    constexpr Elem E = decltype(e)::value;
+    const auto *g = (const elem_t<E>*)dy_dev, *a = (const elem_t<E>*)x_dev;
+    auto* d = (elem_t<E>*)dx_dev;
+    if (!dbias_dev) {
+      const int64_t turn = kDropThreads * kDropItems;
+      const dim3 grid((unsigned)std::min<int64_t>(((int64_t)sh.items + turn - 1) / turn, kMaxGroups));
+      return launch(dropout_kernel<E, true>, grid, kDropThreads, st, sh, rule, a, x_stride, bias_dev, g, dy_stride, d, dx_stride);
+    }
+    if (S > 1) {
+      const int64_t waves = kDropThreads / 64;
+      const dim3 grid((unsigned)std::min<int64_t>(((int64_t)bp.units.units + waves - 1) / waves, kMaxGroups));
+      return launch(dropout_maps_grad_kernel<E>, grid, kDropThreads, st, sh, bp.units, rule, a, x_stride, bias_dev, g, dy_stride, d,
+                    dx_stride, partial);
+    }
+    return launch(dropout_features_grad_kernel<E>, dim3((unsigned)bp.col_blocks, (unsigned)bp.parts), kDropThreads, st, sh, (uint32_t)N,
+                  bp.across_shift, (uint32_t)bp.rows_per_chunk, rule, a, x_stride, bias_dev, g, dy_stride, d, dx_stride, partial);
+  });
+  if (rc || !dbias_dev || bp.parts == 1) return rc;
+  return launch(bias_grad_kernel, sum_grid, kBiasCols * kBiasDown, st, (const float*)partial, (uint32_t)bp.parts, (uint32_t)K, dbias_dev);
+}
+
+int swconv_logprobs_workspace_bytes(int dtype, int64_t rows, int64_t classes, int top, int64_t* bytes) {
+  int64_t stride;
+  if (!bytes) return SWCONV_EINVAL;
+  if (int rc = check_scores(dtype, rows, classes, 0, &stride)) return rc;
+  if (top < 0) return SWCONV_EINVAL;
+  if (top > kTopMax) return SWCONV_EUNSUPPORTED;
+  *bytes = parts_bytes(parts_of(dtype, rows, classes), rows, top);
+  return SWCONV_OK;
+}
+
+int swconv_logprobs_forward(int dtype, int64_t rows, int64_t classes, const void* scores_dev, int64_t row_stride, const int32_t* labels_dev,
+                            int top, void* workspace_dev, int64_t workspace_bytes, void* hip_stream, float* logprob_dev,
+                            float* entropy_dev, float* stats_dev, int32_t* top_class_dev, float* top_logprob_dev) {
+  if (int rc = check_scores(dtype, rows, classes, row_stride, &row_stride)) return rc;
+  if (top < 0) return SWCONV_EINVAL;
+  if (top > kTopMax) return SWCONV_EUNSUPPORTED;
+  if (rows == 0) return SWCONV_OK;
+  const Rows x{scores_dev, rows, classes, row_stride};
+  if (!placed(x, size_of(dtype)) || (logprob_dev && !labels_dev) || (top > 0) != (top_class_dev && top_logprob_dev) ||
+      (!logprob_dev && !entropy_dev && !stats_dev && !top))
+    return SWCONV_EINVAL;
+  for (const void* p : {(const void*)labels_dev, (const void*)logprob_dev, (const void*)entropy_dev, (const void*)stats_dev,
+                        (const void*)top_class_dev, (const void*)top_logprob_dev})
+    if ((uintptr_t)p % 4) return SWCONV_EINVAL;
+  const Parts pt = parts_of(dtype, rows, classes);
+  if (pt.parts > 1 && (!workspace_dev || (uintptr_t)workspace_dev % 16 || workspace_bytes < parts_bytes(pt, rows, top))) return SWCONV_EINVAL;
+  auto* part_sums = (PartSums*)workspace_dev;
+  auto* part_keys = (TopKey*)(part_sums + rows * pt.parts);
+  const LogprobsOut out{logprob_dev, entropy_dev, stats_dev, top_class_dev, top_logprob_dev};
+  const hipStream_t st = (hipStream_t)hip_stream;
+  const StreamDevice device(st);
+  return dispatch_type(dtype, [&](auto e) {
+    constexpr Elem E = decltype(e)::value;
+    constexpr int kWaves = kLogpThreads / 64;
+    const auto* s = (const elem_t<E>*)scores_dev;
+    auto part = [&](auto waves, auto with_top, auto with_entropy) {
+      constexpr int W = decltype(waves)::value;
+      const int64_t groups = (rows * pt.parts + kWaves / W - 1) / (kWaves / W);
+      return launch(logprobs_kernel<E, W, decltype(with_top)::value, decltype(with_entropy)::value>,
+                    dim3((unsigned)std::min(groups, kMaxGroups)), kLogpThreads, st, rows, classes, s, row_stride, labels_dev, top, pt.parts,
+                    pt.part_classes, out, part_sums, part_keys);
+    };
+    auto entropy = [&](auto waves, auto with_top) {
+      return entropy_dev ? part(waves, with_top, std::true_type{}) : part(waves, with_top, std::false_type{});
+    };
+    auto best = [&](auto waves) { return top ? entropy(waves, std::true_type{}) : entropy(waves, std::false_type{}); };
+    const int rc = pt.wave ? best(std::integral_constant<int, 1>{}) : best(std::integral_constant<int, kWaves>{});
+    if (rc || pt.parts == 1) return rc;
+    return launch(logprobs_join_kernel<E>, dim3((unsigned)std::min(rows, kMaxGroups)), 64, st, rows, classes, s, row_stride, labels_dev,
+                  top, pt.parts, out, (const PartSums*)part_sums, (const TopKey*)part_keys);
+  });
+}
+
+int swconv_logprobs_backward(int dtype, int64_t rows, int64_t classes, const void* scores_dev, int64_t row_stride,
+                             const int32_t* labels_dev, const float* stats_dev, const float* entropy_dev, const float* dlogprob_dev,
+                             const float* dentropy_dev, void* hip_stream, void* dscores_dev, int64_t dscores_stride) {
+  if (int rc = check_scores(dtype, rows, classes, row_stride, &row_stride)) return rc;
+  if (int rc = check_scores(dtype, rows, classes, dscores_stride, &dscores_stride)) return rc;
+  if (rows == 0) return SWCONV_OK;
+  const int64_t size = size_of(dtype);
+  const Rows x{scores_dev, rows, classes, row_stride}, dx{dscores_dev, rows, classes, dscores_stride};
+  if (!placed(x, size) || !placed(dx, size) || !may_write(dx, x, size) || !stats_dev || (dlogprob_dev && !labels_dev) ||
+      (dentropy_dev && !entropy_dev) || (!dlogprob_dev && !dentropy_dev))
+    return SWCONV_EINVAL;
+  for (const void* p : {(const void*)labels_dev, (const void*)stats_dev, (const void*)entropy_dev, (const void*)dlogprob_dev,
+                        (const void*)dentropy_dev})
+    if ((uintptr_t)p % 4) return SWCONV_EINVAL;
+  const hipStream_t st = (hipStream_t)hip_stream;
+  const StreamDevice device(st);
+  return dispatch_type(dtype, [&](auto e) {
+    constexpr Elem E = decltype(e)::value;
+    constexpr int V = kLogpVec<E>;
+    const int64_t groups = (classes + V - 1) / V;
+    const int shift = std::min(8, ceil_log2(groups));
+    const int64_t chunks = (groups + (1 << shift) - 1) >> shift, down = kLogpThreads >> shift;
+    const int64_t turns = (rows + down - 1) / down * chunks;
+    return launch(logprobs_grad_kernel<E>, dim3((unsigned)std::min(turns, kMaxGroups)), kLogpThreads, st, rows, classes,
+                  (const elem_t<E>*)scores_dev, row_stride, labels_dev, stats_dev, entropy_dev, dlogprob_dev, dentropy_dev, shift, chunks,
+                  (elem_t<E>*)dscores_dev, dscores_stride);
+  });
+}
+
+}  // extern "C"
