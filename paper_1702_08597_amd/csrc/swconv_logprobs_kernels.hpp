@@ -9,42 +9,108 @@
 // The best t classes, t <= 64: lane i of a wave holds its i-th best as a 64-bit key (score, then the lower class), a
 // score that beats the t-th goes to a list in LDS, and lists of 64 are sorted and merged.
 #pragma once
+#include <type_traits>
 #include "swconv_elements.hpp"
 
 namespace swconv {
 
-constexpr int kLogpThreads = 256;
-constexpr int kLogpUnroll = 2;        // 16-byte loads per lane in flight and tile
+constexpr int kLogpUnroll = 4;        // 16-byte loads per lane and tile
 constexpr int kTopMax = 64;           // one lane each
 constexpr float kFarBelow = -256.0f;  // exp(-256) is 0 in fp32; keeps 0 * inf out of the sums
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
+constexpr float kLowest = -3.402823466e38f;
 
 template <Elem E>
 constexpr int kLogpVec = 16 / sizeof(elem_t<E>);
 
-struct RowSums {
-  float m, s, t;  // largest score, sum of exp(x - m), sum of (x - m) exp(x - m)
-};
-constexpr float kLowest = -3.402823466e38f;
-
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
-__device__ __forceinline__ void rescale(RowSums& a, float m) {
+// ---- lanes ------------------------------------------------------------------------------------------------------
+// The value of lane ^ OFF by moves within the vector unit: a trip through LDS takes ten times as long.
+template <int OFF>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v, int lane) {
+  auto dpp = [](uint32_t a, auto control) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, decltype(control)::value, 0xf, 0xf, true); };
+  using std::integral_constant;
+  if constexpr (OFF == 1) return dpp(v, integral_constant<int, 0xB1>{});         // quad_perm 1 0 3 2
+  else if constexpr (OFF == 2) return dpp(v, integral_constant<int, 0x4E>{});    // quad_perm 2 3 0 1
+  else if constexpr (OFF == 4) return dpp(dpp(v, integral_constant<int, 0x141>{}), integral_constant<int, 0x1B>{});  // 7, then 3
+  else if constexpr (OFF == 7) return dpp(v, integral_constant<int, 0x141>{});   // row_half_mirror
+  else if constexpr (OFF == 8) return dpp(v, integral_constant<int, 0x128>{});   // row_ror 8
+  else if constexpr (OFF == 15) return dpp(v, integral_constant<int, 0x140>{});  // row_mirror
+  else if constexpr (OFF == 16) {
+    const auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return lane & 16 ? s[0] : s[1];
+  } else if constexpr (OFF == 32) {
+    const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return lane & 32 ? s[0] : s[1];
+  } else {
+    static_assert(OFF == 63, "no such exchange");
+    return lane_xor<32>(lane_xor<16>(lane_xor<15>(v, lane), lane), lane);
+  }
+}
+template <int OFF>
+__device__ __forceinline__ float lane_xor(float v, int lane) { return __uint_as_float(lane_xor<OFF>(__float_as_uint(v), lane)); }
+template <int OFF>
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v, int lane) {
+  return (uint64_t)lane_xor<OFF>((uint32_t)(v >> 32), lane) << 32 | lane_xor<OFF>((uint32_t)v, lane);
+}
+template <typename F>
+__device__ __forceinline__ float reduce_lanes(float v, int lane, F&& f) {
+  v = f(v, lane_xor<1>(v, lane));
+  v = f(v, lane_xor<2>(v, lane));
+  v = f(v, lane_xor<7>(v, lane));
+  v = f(v, lane_xor<15>(v, lane));
+  v = f(v, lane_xor<16>(v, lane));
+  return f(v, lane_xor<32>(v, lane));
+}
+
+template <int OFF, typename K>
+__device__ __forceinline__ K exchange(K key, int lane, bool keep_larger) {
+  const K other = lane_xor<OFF>(key, lane);
+  return (other > key) == keep_larger ? other : key;
+}
+template <int OFF, typename K>
+__device__ __forceinline__ K halve(K key, int lane, bool down) {
+  key = exchange<OFF>(key, lane, ((lane & OFF) == 0) == down);
+  if constexpr (OFF > 1) key = halve<OFF / 2>(key, lane, down);
+  return key;
+}
+// 64 keys, one per lane, into descending order
+template <typename K>
+__device__ __forceinline__ K sort_lanes(K key, int lane) {
+  key = halve<1>(key, lane, (lane & 2) == 0);
+  key = halve<2>(key, lane, (lane & 4) == 0);
+  key = halve<4>(key, lane, (lane & 8) == 0);
+  key = halve<8>(key, lane, (lane & 16) == 0);
+  key = halve<16>(key, lane, (lane & 32) == 0);
+  return halve<32>(key, lane, true);
+}
+// the 64 largest of two descending lists, descending
+template <typename K>
+__device__ __forceinline__ K merge_lanes(K a, K b, int lane) {
+  const K mirrored = lane_xor<63>(b, lane);
+  return halve<32>(a > mirrored ? a : mirrored, lane, true);
+}
+
+// ---- the sums of a row ------------------------------------------------------------------------------------------
+// The scores that equal the largest one are counted, not added: a sum that starts at 1 would lose the digits of the
+// others, which are all that is left of ls and H in a row with one likely class.
+struct RowSums {
+  float m;  // the largest score
+  float n;  // how often
+  float s;  // sum of exp(x - m) over the others
+  float t;  // sum of (x - m) exp(x - m)
+};
+
+// Relative to a larger score m.
+__device__ __forceinline__ RowSums raised(const RowSums& a, float m) {
   const float d = fmaxf(a.m - m, kFarBelow), f = exp_fast(d);
-  a.t = f * (a.t + d * a.s);
-  a.s *= f;
-  a.m = m;
+  return {m, 0.0f, f * (a.s + a.n), f * (a.t + d * (a.s + a.n))};
 }
-__device__ __forceinline__ RowSums join(RowSums a, RowSums b) {
+__device__ __forceinline__ RowSums join(const RowSums& a, const RowSums& b) {
   const float m = __builtin_elementwise_maximum(a.m, b.m);
-  rescale(a, m);
-  rescale(b, m);
-  return {m, a.s + b.s, a.t + b.t};
-}
-__device__ __forceinline__ RowSums join_lanes(RowSums a) {
-#pragma unroll
-  for (int off = 32; off; off /= 2) a = join(a, {__shfl_xor(a.m, off), __shfl_xor(a.s, off), __shfl_xor(a.t, off)});
-  return a;
+  const RowSums x = a.m == m ? a : raised(a, m), y = b.m == m ? b : raised(b, m);
+  return {m, x.n + y.n, x.s + y.s, x.t + y.t};
 }
 
 // ---- the best classes -------------------------------------------------------------------------------------------
@@ -60,29 +126,6 @@ __device__ __forceinline__ float top_score(TopKey k) {
 }
 __device__ __forceinline__ int32_t top_index(TopKey k) { return k ? (int32_t)~(uint32_t)k : -1; }
 
-template <typename K>
-__device__ __forceinline__ K exchange(K key, int off, bool keep_larger) {
-  const K other = __shfl_xor(key, off);
-  return keep_larger ? (other > key ? other : key) : (other < key ? other : key);
-}
-// 64 keys, one per lane, into descending order
-template <typename K>
-__device__ __forceinline__ K sort_lanes(K key, int lane) {
-#pragma unroll
-  for (int size = 2; size <= 64; size *= 2)
-#pragma unroll
-    for (int off = size / 2; off; off /= 2) key = exchange(key, off, ((lane & off) == 0) == ((lane & size) == 0));
-  return key;
-}
-// the 64 largest of two descending lists, descending
-__device__ __forceinline__ TopKey merge_lanes(TopKey a, TopKey b, int lane) {
-  const TopKey mirrored = __shfl_xor(b, 63);
-  TopKey key = a > mirrored ? a : mirrored;
-#pragma unroll
-  for (int off = 32; off; off /= 2) key = exchange(key, off, (lane & off) == 0);
-  return key;
-}
-
 struct TopList {
   TopKey best;        // lane i: the i-th best so far
   TopKey* waiting;    // LDS, 128
@@ -97,10 +140,19 @@ struct TopList {
     score = -INFINITY;
     index = -1;
   }
+  // The t-th largest of 64 lanes' largest scores is no larger than the t-th best: nearly all scores fall below it.
+  __device__ __forceinline__ void guess(float lane_max, int lane, int top) {
+    const float bar = __shfl(sort_lanes(lane_max, lane), top - 1);
+    if (bar > -INFINITY) {
+      score = bar;
+      index = INT32_MAX;
+    }
+  }
   __device__ __forceinline__ void take(int lane, int top) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     const int n = min(count, 64);
-    best = merge_lanes(best, sort_lanes(lane < n ? waiting[lane] : (TopKey)0, lane), lane);
+    const TopKey sorted = sort_lanes(lane < n ? waiting[lane] : (TopKey)0, lane);
+    best = merge_lanes(best, sorted, lane);
     const TopKey rest = lane < count - 64 ? waiting[64 + lane] : (TopKey)0;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     if (lane < count - 64) waiting[lane] = rest;
@@ -114,6 +166,7 @@ struct TopList {
   }
   // one score from each lane
   __device__ __forceinline__ void offer(float x, int32_t j, int lane, int top) {
+    if (__ballot(x >= score) == 0) return;
     const bool hit = x > score || (x == score && j < index);
     const uint64_t hits = __ballot(hit);
     if (hits == 0) return;
@@ -133,10 +186,10 @@ struct LogprobsOut {
 // A row's results from its sums and its best classes; called by one wave.
 template <Elem E>
 __device__ __forceinline__ void finish_row(const LogprobsOut& out, const elem_t<E>* scores, int64_t row_stride, int64_t classes,
-                                           const int32_t* labels, int64_t row, RowSums a, TopKey best, int top, int lane) {
+                                           const int32_t* labels, int64_t row, const RowSums& a, TopKey best, int top, int lane) {
   const bool poisoned = !(a.m <= -kLowest);  // NaN or +inf among the scores
-  const bool empty = a.s == 0.0f && !poisoned;
-  const float ls = empty ? 0.0f : poisoned ? NAN : logf(a.s);
+  const bool empty = a.n == 0.0f && !poisoned;
+  const float ls = empty ? 0.0f : poisoned ? NAN : a.n == 1.0f ? log1pf(a.s) : logf(a.n + a.s);
   const float m = empty ? -INFINITY : poisoned ? NAN : a.m;
   if (lane == 0) {
     if (out.logprob) {
@@ -148,7 +201,7 @@ __device__ __forceinline__ void finish_row(const LogprobsOut& out, const elem_t<
         lp = empty ? -INFINITY : ((float)scores[row * row_stride + label] - m) - ls;
       out.logprob[row] = lp;
     }
-    if (out.entropy) out.entropy[row] = empty ? 0.0f : poisoned ? NAN : ls - a.t / a.s;
+    if (out.entropy) out.entropy[row] = empty ? 0.0f : poisoned ? NAN : ls - a.t / (a.n + a.s);
     if (out.stats) {
       out.stats[2 * row] = m;
       out.stats[2 * row + 1] = ls;
@@ -160,18 +213,32 @@ __device__ __forceinline__ void finish_row(const LogprobsOut& out, const elem_t<
   }
 }
 
-// Parts of rows whose results wait for their join, in the workspace.
-struct PartSums {
-  float m, s, t, unused;
-};
+// The waves of a workgroup join theirs in a tree; wave 0 has the result.  Ends with LDS free for the next turn.
+template <int WAVES, bool TOP>
+__device__ __forceinline__ void join_waves(RowSums& a, TopKey& best, RowSums* lds_sums, TopKey (*lds_keys)[128], int wave, int lane) {
+#pragma unroll
+  for (int half = WAVES / 2; half; half /= 2) {
+    if (wave >= half && wave < 2 * half) {
+      if (lane == 0) lds_sums[wave] = a;
+      if constexpr (TOP) lds_keys[wave][lane] = best;
+    }
+    __syncthreads();
+    if (wave < half) {
+      a = join(a, lds_sums[wave + half]);
+      if constexpr (TOP) best = merge_lanes(best, lds_keys[wave + half][lane], lane);
+    }
+  }
+}
 
-// WAVES waves of a workgroup share a part of a row, tile by tile (a tile: kLogpUnroll 16-byte loads from each lane).
+// WAVES waves share a part of a row, tile by tile (a tile: kLogpUnroll 16-byte loads from each lane).  All lanes of a
+// wave keep their sums relative to one score, the largest that the wave has seen: it changes in every i-th tile or so,
+// and the other tiles take no scaling.
 template <Elem E, int WAVES, bool TOP, bool ENTROPY>
-__global__ __launch_bounds__(kLogpThreads) void logprobs_kernel(int64_t rows, int64_t classes, const elem_t<E>* __restrict__ scores,
+__global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void logprobs_kernel(int64_t rows, int64_t classes, const elem_t<E>* __restrict__ scores,
                                                                 int64_t row_stride, const int32_t* __restrict__ labels, int top,
                                                                 int parts, int64_t part_classes, LogprobsOut out,
-                                                                PartSums* __restrict__ part_sums, TopKey* __restrict__ part_keys) {
-  constexpr int V = kLogpVec<E>, U = kLogpUnroll, kWaves = kLogpThreads / 64, kTile = 64 * V * U;
+                                                                RowSums* __restrict__ part_sums, TopKey* __restrict__ part_keys) {
+  constexpr int V = kLogpVec<E>, U = kLogpUnroll, kWaves = WAVES > 4 ? WAVES : 4, kTile = 64 * V * U;
   __shared__ TopKey lists[TOP ? kWaves : 1][128];
   __shared__ RowSums wave_sums[kWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part_wave = wave % WAVES;
@@ -179,7 +246,7 @@ __global__ __launch_bounds__(kLogpThreads) void logprobs_kernel(int64_t rows, in
   const int64_t n_parts = rows * parts;
   for (int64_t group = blockIdx.x; group * kPartsPerGroup < n_parts; group += gridDim.x) {
     const int64_t id = group * kPartsPerGroup + wave / WAVES;
-    RowSums a{kLowest, 0.0f, 0.0f};
+    RowSums a{kLowest, 0.0f, 0.0f, 0.0f};
     TopList list;
     if constexpr (TOP) list.start(lists[wave]);
     const int64_t row = parts == 1 ? id : id / parts;
@@ -187,15 +254,21 @@ __global__ __launch_bounds__(kLogpThreads) void logprobs_kernel(int64_t rows, in
       const int64_t begin = parts == 1 ? 0 : (id - row * parts) * part_classes;
       const int64_t end = min(classes, begin + part_classes);
       const elem_t<E>* x_row = scores + row * row_stride;
+      bool first = true;
       for (int64_t tile = begin + (int64_t)part_wave * kTile; tile < end; tile += (int64_t)WAVES * kTile) {
         Pack<E, V> raw[U];
+        if (tile + kTile <= end) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int64_t j = tile + (u * 64 + lane) * V;
-          if (j + V <= end)
-            raw[u] = load_pack<E, V>(x_row + j);
-          else
-            raw[u] = load_part<E, V>(x_row + j, (int)max((int64_t)0, end - j), -INFINITY);
+          for (int u = 0; u < U; ++u) raw[u] = stream_pack<E, V>(x_row + tile + (u * 64 + lane) * V);
+        } else {
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int64_t j = tile + (u * 64 + lane) * V;
+            if (j + V <= end)
+              raw[u] = load_pack<E, V>(x_row + j);
+            else
+              raw[u] = load_part<E, V>(x_row + j, (int)max((int64_t)0, end - j), -INFINITY);
+          }
         }
         float group_max[U];
 #pragma unroll
@@ -204,87 +277,100 @@ __global__ __launch_bounds__(kLogpThreads) void logprobs_kernel(int64_t rows, in
 #pragma unroll
           for (int i = 1; i < V; ++i) group_max[u] = __builtin_elementwise_maximum(group_max[u], (float)raw[u].v[i]);
         }
-        float m = a.m;
+        float lane_max = group_max[0];
 #pragma unroll
-        for (int u = 0; u < U; ++u) m = __builtin_elementwise_maximum(m, group_max[u]);
-        rescale(a, m);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            const float d = fmaxf((float)raw[u].v[i] - m, kFarBelow), e = exp_fast(d);
-            a.s += e;
-            if constexpr (ENTROPY) a.t += d * e;
-          }
-        if constexpr (TOP) {
+        for (int u = 1; u < U; ++u) lane_max = __builtin_elementwise_maximum(lane_max, group_max[u]);
+        if (__ballot(!(lane_max < a.m)) == 0) {
 #pragma unroll
           for (int u = 0; u < U; ++u)
-            if (__ballot(group_max[u] >= list.score))
 #pragma unroll
-              for (int i = 0; i < V; ++i) list.offer((float)raw[u].v[i], (int32_t)(tile + (u * 64 + lane) * V + i), lane, top);
+            for (int i = 0; i < V; ++i) {
+              const float d = fmaxf((float)raw[u].v[i] - a.m, kFarBelow), e = exp_fast(d);
+              a.s += e;
+              if constexpr (ENTROPY) a.t += d * e;
+            }
+        } else {
+          const float m = reduce_lanes(__builtin_elementwise_maximum(lane_max, a.m), lane, [](float x, float y) { return __builtin_elementwise_maximum(x, y); });
+          if (!(m == a.m)) a = raised(a, m);
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+              const float x = (float)raw[u].v[i], d = fmaxf(x - m, kFarBelow), e = exp_fast(d);
+              a.n += x == m ? 1.0f : 0.0f;
+              a.s += x == m ? 0.0f : e;
+              if constexpr (ENTROPY) a.t += d * e;
+            }
+        }
+        if constexpr (TOP) {
+          if (first) list.guess(lane_max, lane, top);
+          first = false;
+          if (__ballot(lane_max >= list.score)) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+              if (__ballot(group_max[u] >= list.score))
+#pragma unroll
+                for (int i = 0; i < V; ++i) list.offer((float)raw[u].v[i], (int32_t)(tile + (u * 64 + lane) * V + i), lane, top);
+          }
         }
       }
     }
-    a = join_lanes(a);
+    auto add = [](float x, float y) { return x + y; };
+    a.n = reduce_lanes(a.n, lane, add);
+    a.s = reduce_lanes(a.s, lane, add);
+    if constexpr (ENTROPY) a.t = reduce_lanes(a.t, lane, add);
     if constexpr (TOP) list.take(lane, top);
     if constexpr (WAVES > 1) {
       static_assert(WAVES == kWaves, "one part per workgroup");
-      if (lane == 0) wave_sums[wave] = a;
-      if constexpr (TOP) lists[wave][lane] = list.best;
-      __syncthreads();
-      if (wave == 0) {
-        for (int w = 1; w < WAVES; ++w) {
-          a = join(a, wave_sums[w]);
-          if constexpr (TOP) list.best = merge_lanes(list.best, lists[w][lane], lane);
-        }
-      }
-      __syncthreads();
+      join_waves<WAVES, TOP>(a, list.best, wave_sums, lists, wave, lane);
     }
     if (part_wave == 0 && id < n_parts) {
       if (parts == 1) {
         finish_row<E>(out, scores, row_stride, classes, labels, row, a, TOP ? list.best : 0, top, lane);
       } else {
-        if (lane == 0) part_sums[id] = {a.m, a.s, a.t, 0.0f};
+        if (lane == 0) part_sums[id] = a;
         if constexpr (TOP)
           if (lane < top) part_keys[id * top + lane] = list.best;
       }
     }
+    if constexpr (WAVES > 1) __syncthreads();  // wave 0 has read the last list
   }
 }
 
-// Joins the parts of a row: a wave per row.
+// Joins the parts of a row: a workgroup per row, its waves take every fourth part.
 template <Elem E>
-__global__ __launch_bounds__(64) void logprobs_join_kernel(int64_t rows, int64_t classes, const elem_t<E>* __restrict__ scores,
+__global__ __launch_bounds__(256) void logprobs_join_kernel(int64_t rows, int64_t classes, const elem_t<E>* __restrict__ scores,
                                                            int64_t row_stride, const int32_t* __restrict__ labels, int top, int parts,
-                                                           LogprobsOut out, const PartSums* __restrict__ part_sums,
+                                                           LogprobsOut out, const RowSums* __restrict__ part_sums,
                                                            const TopKey* __restrict__ part_keys) {
-  const int lane = threadIdx.x;
+  __shared__ TopKey lists[4][128];
+  __shared__ RowSums wave_sums[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-    RowSums a{kLowest, 0.0f, 0.0f};
-    for (int p = lane; p < parts; p += 64) {
-      const PartSums b = part_sums[row * parts + p];
-      a = join(a, {b.m, b.s, b.t});
-    }
-    a = join_lanes(a);
+    RowSums a{kLowest, 0.0f, 0.0f, 0.0f};
     TopKey best = 0;
-    if (top)
-      for (int p = 0; p < parts; ++p)
-        best = merge_lanes(best, lane < top ? part_keys[(row * parts + p) * top + lane] : (TopKey)0, lane);
-    finish_row<E>(out, scores, row_stride, classes, labels, row, a, best, top, lane);
+    for (int p = wave; p < parts; p += 4) {
+      a = join(a, part_sums[row * parts + p]);
+      if (top) best = merge_lanes(best, lane < top ? part_keys[(row * parts + p) * top + lane] : (TopKey)0, lane);
+    }
+    join_waves<4, true>(a, best, wave_sums, lists, wave, lane);
+    if (wave == 0) finish_row<E>(out, scores, row_stride, classes, labels, row, a, best, top, lane);
+    __syncthreads();
   }
 }
 
 // ---- backward ---------------------------------------------------------------------------------------------------
 // `across` threads (a power of two) share a row or, of a long row, a chunk; a thread takes one 16-byte group.
+constexpr int kGradThreads = 256;
 template <Elem E>
-__global__ __launch_bounds__(kLogpThreads) void logprobs_grad_kernel(int64_t rows, int64_t classes, const elem_t<E>* scores,
+__global__ __launch_bounds__(kGradThreads) void logprobs_grad_kernel(int64_t rows, int64_t classes, const elem_t<E>* scores,
                                                                      int64_t row_stride, const int32_t* __restrict__ labels,
                                                                      const float* __restrict__ stats, const float* __restrict__ entropy,
                                                                      const float* __restrict__ dlogprob,
                                                                      const float* __restrict__ dentropy, int across_shift,
                                                                      int64_t chunks, elem_t<E>* out, int64_t out_stride) {
   constexpr int V = kLogpVec<E>;
-  const int across = 1 << across_shift, down = kLogpThreads >> across_shift;
+  const int across = 1 << across_shift, down = kGradThreads >> across_shift;
   const int64_t turns = (rows + down - 1) / down * chunks;
   for (int64_t turn = blockIdx.x; turn < turns; turn += gridDim.x) {
     const int64_t row0 = chunks == 1 ? turn : turn / chunks;

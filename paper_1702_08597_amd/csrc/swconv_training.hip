@@ -153,23 +153,23 @@ int check_scores(int dtype, int64_t rows, int64_t classes, int64_t given, int64_
   return rows > kMost || *stride > kMost || (rows > 1 && rows - 1 > kMost / *stride) ? SWCONV_EUNSUPPORTED : SWCONV_OK;
 }
 
-// One wave takes rows of up to 2048 classes; longer ones a workgroup, and where there are few rows several.
 struct Parts {
-  bool wave;
-  int parts;
+  int waves, parts;
   int64_t part_classes;
 };
 Parts parts_of(int dtype, int64_t rows, int64_t classes) {
-  if (classes <= 2048) return {true, 1, classes};
-  const int64_t tile = 4 * 64 * (16 / size_of(dtype)) * kLogpUnroll;
-  int64_t parts = std::clamp<int64_t>(1024 / std::max<int64_t>(rows, 1), 1, std::max<int64_t>(1, classes / (4 * tile)));
+  const int64_t tile = 64 * (16 / size_of(dtype)) * kLogpUnroll;
+  if (classes <= 2 * tile) return {1, 1, classes};
+  if (rows > 256) return {4, 1, classes};
+  if (classes <= 32 * tile) return {16, 1, classes};
+  int64_t parts = std::clamp<int64_t>(512 / std::max<int64_t>(rows, 1), 1, std::max<int64_t>(1, classes / (16 * tile)));
   parts = std::min<int64_t>(parts, 64);
   int64_t part = (classes + parts - 1) / parts;
   part = (part + tile - 1) / tile * tile;
-  return {false, (int)((classes + part - 1) / part), part};
+  return {16, (int)((classes + part - 1) / part), part};
 }
 int64_t parts_bytes(const Parts& p, int64_t rows, int top) {
-  return p.parts == 1 ? 0 : rows * p.parts * ((int64_t)sizeof(PartSums) + top * (int64_t)sizeof(TopKey));
+  return p.parts == 1 ? 0 : rows * p.parts * ((int64_t)sizeof(RowSums) + top * (int64_t)sizeof(TopKey));
 }
 
 }  // namespace
@@ -284,30 +284,33 @@ int swconv_logprobs_forward(int dtype, int64_t rows, int64_t classes, const void
     if ((uintptr_t)p % 4) return SWCONV_EINVAL;
   const Parts pt = parts_of(dtype, rows, classes);
   if (pt.parts > 1 && (!workspace_dev || (uintptr_t)workspace_dev % 16 || workspace_bytes < parts_bytes(pt, rows, top))) return SWCONV_EINVAL;
-  auto* part_sums = (PartSums*)workspace_dev;
+  auto* part_sums = (RowSums*)workspace_dev;
   auto* part_keys = (TopKey*)(part_sums + rows * pt.parts);
   const LogprobsOut out{logprob_dev, entropy_dev, stats_dev, top_class_dev, top_logprob_dev};
   const hipStream_t st = (hipStream_t)hip_stream;
   const StreamDevice device(st);
   return dispatch_type(dtype, [&](auto e) {
     constexpr Elem E = decltype(e)::value;
-    constexpr int kWaves = kLogpThreads / 64;
     const auto* s = (const elem_t<E>*)scores_dev;
     auto part = [&](auto waves, auto with_top, auto with_entropy) {
       constexpr int W = decltype(waves)::value;
-      const int64_t groups = (rows * pt.parts + kWaves / W - 1) / (kWaves / W);
+      constexpr int kRows = W < 4 ? 4 / W : 1;  // parts of a workgroup
+      const int64_t groups = (rows * pt.parts + kRows - 1) / kRows;
       return launch(logprobs_kernel<E, W, decltype(with_top)::value, decltype(with_entropy)::value>,
-                    dim3((unsigned)std::min(groups, kMaxGroups)), kLogpThreads, st, rows, classes, s, row_stride, labels_dev, top, pt.parts,
+                    dim3((unsigned)std::min(groups, kMaxGroups)), W < 4 ? 256 : W * 64, st, rows, classes, s, row_stride, labels_dev, top, pt.parts,
                     pt.part_classes, out, part_sums, part_keys);
     };
     auto entropy = [&](auto waves, auto with_top) {
       return entropy_dev ? part(waves, with_top, std::true_type{}) : part(waves, with_top, std::false_type{});
     };
     auto best = [&](auto waves) { return top ? entropy(waves, std::true_type{}) : entropy(waves, std::false_type{}); };
-    const int rc = pt.wave ? best(std::integral_constant<int, 1>{}) : best(std::integral_constant<int, kWaves>{});
+    using std::integral_constant;
+    const int rc = pt.waves == 1   ? best(integral_constant<int, 1>{})
+                   : pt.waves == 4 ? best(integral_constant<int, 4>{})
+                                   : best(integral_constant<int, 16>{});
     if (rc || pt.parts == 1) return rc;
-    return launch(logprobs_join_kernel<E>, dim3((unsigned)std::min(rows, kMaxGroups)), 64, st, rows, classes, s, row_stride, labels_dev,
-                  top, pt.parts, out, (const PartSums*)part_sums, (const TopKey*)part_keys);
+    return launch(logprobs_join_kernel<E>, dim3((unsigned)std::min(rows, kMaxGroups)), 256, st, rows, classes, s, row_stride, labels_dev,
+                  top, pt.parts, out, (const RowSums*)part_sums, (const TopKey*)part_keys);
   });
 }
 
@@ -332,9 +335,9 @@ int swconv_logprobs_backward(int dtype, int64_t rows, int64_t classes, const voi
     constexpr int V = kLogpVec<E>;
     const int64_t groups = (classes + V - 1) / V;
     const int shift = std::min(8, ceil_log2(groups));
-    const int64_t chunks = (groups + (1 << shift) - 1) >> shift, down = kLogpThreads >> shift;
+    const int64_t chunks = (groups + (1 << shift) - 1) >> shift, down = kGradThreads >> shift;
     const int64_t turns = (rows + down - 1) / down * chunks;
-    return launch(logprobs_grad_kernel<E>, dim3((unsigned)std::min(turns, kMaxGroups)), kLogpThreads, st, rows, classes,
+    return launch(logprobs_grad_kernel<E>, dim3((unsigned)std::min(turns, kMaxGroups)), kGradThreads, st, rows, classes,
                   (const elem_t<E>*)scores_dev, row_stride, labels_dev, stats_dev, entropy_dev, dlogprob_dev, dentropy_dev, shift, chunks,
                   (elem_t<E>*)dscores_dev, dscores_stride);
   });
