@@ -39,13 +39,55 @@ __device__ __forceinline__ Pack<E, V> load_pack(const elem_t<E>* p) {
   return a;
 }
 
-// 16 bytes of a stream that is read once: without the hint a read of 1 GB runs at 6.3 TB/s, with it at 7.0, a copy at 6.2
-// and, hinted on both sides, 6.5.
-typedef uint32_t Stream16 __attribute__((ext_vector_type(4), aligned(2)));
-template <Elem E, int V>
-__device__ __forceinline__ Pack<E, V> stream_pack(const elem_t<E>* p) {
-  static_assert(sizeof(Pack<E, V>) == 16, "one access");
-  return __builtin_bit_cast(Pack<E, V>, (Stream16)__builtin_nontemporal_load(reinterpret_cast<const Stream16*>(p)));
+// 16 bytes of a row as words, so that an element is one operation away from its float.
+typedef uint32_t Words __attribute__((ext_vector_type(4)));
+typedef uint32_t LooseWords __attribute__((ext_vector_type(4), aligned(2)));
+template <Elem E>
+constexpr int kWordsElems = 16 / sizeof(elem_t<E>);
+
+template <Elem E>
+__device__ __forceinline__ float word_elem(const Words& w, int i) {
+  if constexpr (E == Elem::f32) return __uint_as_float(w[i]);
+  if constexpr (E == Elem::bf16) return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  if constexpr (E == Elem::f16) return (float)__builtin_bit_cast(_Float16, (uint16_t)(w[i / 2] >> (i % 2 * 16)));
+}
+// `once`: nothing reads these bytes again soon.  With the hint a read of 1 GB runs at 7.0 TB/s, without at 6.3.
+template <Elem E>
+__device__ __forceinline__ Words load_words(const elem_t<E>* p, bool once) {
+  const auto* q = reinterpret_cast<const LooseWords*>(p);
+  return once ? (Words)__builtin_nontemporal_load(q) : (Words)*q;
+}
+template <Elem E>
+constexpr uint32_t kMinusInf = E == Elem::f32 ? 0xff800000u : E == Elem::bf16 ? 0xff80u : 0xfc00u;
+// The first n elements of a row that is shorter than 16 bytes, -inf behind them.
+template <Elem E>
+__device__ __forceinline__ Words load_words_part(const elem_t<E>* p, int n) {
+  Words w;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if constexpr (E == Elem::f32) {
+      w[k] = k < n ? __float_as_uint(p[k]) : kMinusInf<E>;
+    } else {
+      const uint32_t lo = 2 * k < n ? __builtin_bit_cast(uint16_t, p[2 * k]) : kMinusInf<E>;
+      const uint32_t hi = 2 * k + 1 < n ? __builtin_bit_cast(uint16_t, p[2 * k + 1]) : kMinusInf<E>;
+      w[k] = hi << 16 | lo;
+    }
+  }
+  return w;
+}
+// -inf in place of the first n elements.
+template <Elem E>
+__device__ __forceinline__ Words without_first(Words w, int n) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if constexpr (E == Elem::f32) {
+      w[k] = k < n ? kMinusInf<E> : w[k];
+    } else {
+      const uint32_t lo = 2 * k < n ? kMinusInf<E> : w[k] & 0xffffu;
+      w[k] = 2 * k + 1 < n ? kMinusInf<E> << 16 | lo : (w[k] & 0xffff0000u) | lo;
+    }
+  }
+  return w;
 }
 
 // The first n of V elements (n < V), `fill` behind them.

@@ -6,8 +6,10 @@
 //   d x_j = g ([j = label] - p_j) - h p_j (log p_j + H)
 // A class of score -inf is masked: exp gives 0, and it never is among the best.  NaN and +inf make the row's largest
 // score NaN or +inf (the maximum used propagates NaN), from which the row's results are made NaN.
-// The best t classes, t <= 64: lane i of a wave holds its i-th best as a 64-bit key (score, then the lower class), a
-// score that beats the t-th goes to a list in LDS, and lists of 64 are sorted and merged.
+// The best t classes, t <= 64: the pass over the scores only notes the largest one of each lane and segment (16 to a wave's
+// share of a row).  The t-th largest of the lanes' largest scores is a bar that t scores reach and few others: the lanes and
+// segments that reach it are read again, a lane to a score, and what reaches it is sorted, as 64-bit keys (score, then
+// the lower class), one to a lane.
 #pragma once
 #include <type_traits>
 #include "swconv_elements.hpp"
@@ -19,9 +21,6 @@ constexpr int kTopMax = 64;           // one lane each
 constexpr float kFarBelow = -256.0f;  // exp(-256) is 0 in fp32; keeps 0 * inf out of the sums
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 constexpr float kLowest = -3.402823466e38f;
-
-template <Elem E>
-constexpr int kLogpVec = 16 / sizeof(elem_t<E>);
 
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
@@ -54,6 +53,10 @@ template <int OFF>
 __device__ __forceinline__ uint64_t lane_xor(uint64_t v, int lane) {
   return (uint64_t)lane_xor<OFF>((uint32_t)(v >> 32), lane) << 32 | lane_xor<OFF>((uint32_t)v, lane);
 }
+// The calling lane's number among those of a mask.
+__device__ __forceinline__ int lanes_below(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
 template <typename F>
 __device__ __forceinline__ float reduce_lanes(float v, int lane, F&& f) {
   v = f(v, lane_xor<1>(v, lane));
@@ -75,13 +78,15 @@ __device__ __forceinline__ K halve(K key, int lane, bool down) {
   if constexpr (OFF > 1) key = halve<OFF / 2>(key, lane, down);
   return key;
 }
-// 64 keys, one per lane, into descending order
+// 64 keys, one per lane, into descending order; `n`: keys behind lane n - 1 are all 0 (only the first 16 lanes, half of
+// the steps, where that says so)
 template <typename K>
-__device__ __forceinline__ K sort_lanes(K key, int lane) {
+__device__ __forceinline__ K sort_lanes(K key, int lane, int n) {
   key = halve<1>(key, lane, (lane & 2) == 0);
   key = halve<2>(key, lane, (lane & 4) == 0);
   key = halve<4>(key, lane, (lane & 8) == 0);
   key = halve<8>(key, lane, (lane & 16) == 0);
+  if (n <= 16) return key;
   key = halve<16>(key, lane, (lane & 32) == 0);
   return halve<32>(key, lane, true);
 }
@@ -99,13 +104,20 @@ struct RowSums {
   float m;  // the largest score
   float n;  // how often
   float s;  // sum of exp(x - m) over the others
-  float t;  // sum of (x - m) exp(x - m)
+  float t;  // sum of log2(exp(x - m)) exp(x - m)
 };
 
-// Relative to a larger score m.
+// exp(x - m) for x < m as 2^(x log2 e - c) with c = m log2 e rounded: one fused multiply-add whose only error is its own
+// rounding; what c is off by (less than 64) is put right once per row (finish_row).  From 2^30 on the next lower score is 128
+// further down, where exp gives 0: so does c = inf.
+__device__ __forceinline__ float reference(float m) { return fabsf(m) >= 1073741824.0f ? INFINITY : m * kLog2e; }
+
+// The sums relative to a larger score m, which makes the scores that were largest ordinary ones.
 __device__ __forceinline__ RowSums raised(const RowSums& a, float m) {
-  const float d = fmaxf(a.m - m, kFarBelow), f = exp_fast(d);
-  return {m, 0.0f, f * (a.s + a.n), f * (a.t + d * (a.s + a.n))};
+  const float c = reference(m);
+  const float d = fmaxf(fminf(reference(a.m) - c, 0.0f), kFarBelow), f = __builtin_amdgcn_exp2f(d);
+  const float d_n = fmaxf(__builtin_fmaf(a.m, kLog2e, -c), kFarBelow), n = a.n * __builtin_amdgcn_exp2f(d_n);
+  return {m, 0.0f, f * a.s + n, f * (a.t + d * a.s) + d_n * n};
 }
 __device__ __forceinline__ RowSums join(const RowSums& a, const RowSums& b) {
   const float m = __builtin_elementwise_maximum(a.m, b.m);
@@ -126,37 +138,34 @@ __device__ __forceinline__ float top_score(TopKey k) {
 }
 __device__ __forceinline__ int32_t top_index(TopKey k) { return k ? (int32_t)~(uint32_t)k : -1; }
 
-struct TopList {
-  TopKey best;        // lane i: the i-th best so far
-  TopKey* waiting;    // LDS, 128
-  int count;          // of them
-  float score;        // what a score has to beat: the t-th best's,
-  int32_t index;      // or equal it at a lower class
+constexpr int kSegments = 16;
+constexpr int kWaiting = 128;  // a list in LDS: fewer than 64 and 64 more
 
-  __device__ __forceinline__ void start(TopKey* lds) {
+struct TopList {
+  TopKey best;        // lane i: the i-th best so far, if any
+  TopKey* waiting;    // LDS, kWaiting
+  int count;          // of them, fewer than 64 between calls
+  bool any;           // best holds some
+  float score;        // what a score has to beat,
+  int32_t index;      // or equal at a lower class
+
+  __device__ __forceinline__ void start(TopKey* lds, float bar) {
     best = 0;
     waiting = lds;
     count = 0;
-    score = -INFINITY;
-    index = -1;
+    any = false;
+    score = bar;
+    index = INT32_MAX;
   }
-  // The t-th largest of 64 lanes' largest scores is no larger than the t-th best: nearly all scores fall below it.
-  __device__ __forceinline__ void guess(float lane_max, int lane, int top) {
-    const float bar = __shfl(sort_lanes(lane_max, lane), top - 1);
-    if (bar > -INFINITY) {
-      score = bar;
-      index = INT32_MAX;
-    }
-  }
+  // Sorts what waits into the best.
   __device__ __forceinline__ void take(int lane, int top) {
+    if (count == 0) return;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     const int n = min(count, 64);
-    const TopKey sorted = sort_lanes(lane < n ? waiting[lane] : (TopKey)0, lane);
-    best = merge_lanes(best, sorted, lane);
-    const TopKey rest = lane < count - 64 ? waiting[64 + lane] : (TopKey)0;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (lane < count - 64) waiting[lane] = rest;
     count -= n;
+    const TopKey sorted = sort_lanes(lane < n ? waiting[count + lane] : (TopKey)0, lane, n);
+    best = any ? merge_lanes(best, sorted, lane) : sorted;
+    any = true;
     const TopKey bar = __shfl(best, top - 1);
     if (bar) {
       score = top_score(bar);
@@ -164,17 +173,50 @@ struct TopList {
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
-  // one score from each lane
+  // One score from each lane.
   __device__ __forceinline__ void offer(float x, int32_t j, int lane, int top) {
-    if (__ballot(x >= score) == 0) return;
     const bool hit = x > score || (x == score && j < index);
     const uint64_t hits = __ballot(hit);
-    if (hits == 0) return;
-    if (hit) waiting[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(hits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hits, 0))] = top_key(x, j);
+    if (hit) waiting[count + lanes_below(hits)] = top_key(x, j);
     count += __popcll(hits);
     if (count >= 64) take(lane, top);
   }
 };
+
+// Calls see(score or -inf, class) for one score to a lane, for all that a wave's lanes hold in segments whose largest score
+// reaches bar(): a lane's scores of a tile are U runs of V.  `owners`: LDS, room for 128 (segment, lane) pairs; all of
+// them are read in one go, 64 scores at a time and four such reads in flight.
+template <Elem E, typename Bar, typename See>
+__device__ __forceinline__ void look_again(const elem_t<E>* x_row, const float (*segment_max)[64], uint16_t* owners, int segments,
+                                           int segment_tiles, int64_t first, int64_t step, int64_t end, int lane, Bar&& bar, See&& see) {
+  constexpr int V = kWordsElems<E>, U = kLogpUnroll, kFlight = 4;
+  int n = 0;
+  for (int s = 0; s < segments; ++s) {
+    const bool reaches = segment_max[s][lane] >= bar();
+    const uint64_t reaching = __ballot(reaches);
+    if (reaches) owners[n + lanes_below(reaching)] = (uint16_t)(s << 6 | lane);
+    n += __popcll(reaching);
+    if (n == 0 || (n < 64 && s + 1 < segments)) continue;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int i = 0; i < segment_tiles; ++i)
+      for (int q0 = 0; q0 < n * (U * V); q0 += 64 * kFlight) {
+        float x[kFlight];
+        int64_t j[kFlight];
+#pragma unroll
+        for (int f = 0; f < kFlight; ++f) {
+          const int q = q0 + 64 * f + lane, in_tile = q % (U * V);
+          const int owner = q < n * (U * V) ? owners[q / (U * V)] : 0;
+          j[f] = first + ((int64_t)(owner >> 6) * segment_tiles + i) * step + (in_tile / V * 64 + (owner & 63)) * V + in_tile % V;
+          x[f] = q < n * (U * V) && j[f] < end ? (float)x_row[j[f]] : -INFINITY;
+        }
+#pragma unroll
+        for (int f = 0; f < kFlight; ++f)
+          if (q0 + 64 * f < n * (U * V)) see(x[f], (int32_t)j[f]);
+      }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    n = 0;
+  }
+}
 
 // ---- forward ----------------------------------------------------------------------------------------------------
 struct LogprobsOut {
@@ -183,25 +225,34 @@ struct LogprobsOut {
   float* top_logprob;
 };
 
+// The class asked for (below 0: none) and its score, NaN where there is no such class.
+struct Label {
+  int32_t at;
+  float score;
+};
+template <Elem E>
+__device__ __forceinline__ Label label_at(int32_t at, const elem_t<E>* x_row, int64_t classes) {
+  return {at, at < 0 ? 0.0f : at < classes ? (float)x_row[at] : NAN};
+}
+
 // A row's results from its sums and its best classes; called by one wave.
 template <Elem E>
-__device__ __forceinline__ void finish_row(const LogprobsOut& out, const elem_t<E>* scores, int64_t row_stride, int64_t classes,
-                                           const int32_t* labels, int64_t row, const RowSums& a, TopKey best, int top, int lane) {
+__device__ __forceinline__ void finish_row(const LogprobsOut& out,
+                                           int64_t row, Label label, const RowSums& a, TopKey best, int top, int lane) {
   const bool poisoned = !(a.m <= -kLowest);  // NaN or +inf among the scores
   const bool empty = a.n == 0.0f && !poisoned;
-  const float ls = empty ? 0.0f : poisoned ? NAN : a.n == 1.0f ? log1pf(a.s) : logf(a.n + a.s);
+  // m log2 e = c + off: every exponential, 2^(x log2 e - c), is 2^off too large, its logarithm off too high
+  const float c = reference(a.m), off = isinf(c) ? 0.0f : __builtin_fmaf(a.m, kLog2e, -c), back = __builtin_amdgcn_exp2f(-off);
+  const float s = a.s * back, t = kLn2 * (a.t - off * a.s) * back;
+  const float ls = empty ? 0.0f : poisoned ? NAN : a.n == 1.0f ? log1pf(s) : logf(a.n + s);
   const float m = empty ? -INFINITY : poisoned ? NAN : a.m;
   if (lane == 0) {
     if (out.logprob) {
-      const int32_t label = labels[row];
-      float lp = NAN;
-      if (label < 0)
-        lp = 0.0f;
-      else if (label < classes)
-        lp = empty ? -INFINITY : ((float)scores[row * row_stride + label] - m) - ls;
+      float lp = label.score;
+      if (label.at >= 0) lp = empty && lp == lp ? -INFINITY : (lp - m) - ls;
       out.logprob[row] = lp;
     }
-    if (out.entropy) out.entropy[row] = empty ? 0.0f : poisoned ? NAN : ls - a.t / (a.n + a.s);
+    if (out.entropy) out.entropy[row] = empty ? 0.0f : poisoned ? NAN : ls - t / (a.n + s);
     if (out.stats) {
       out.stats[2 * row] = m;
       out.stats[2 * row + 1] = ls;
@@ -213,20 +264,61 @@ __device__ __forceinline__ void finish_row(const LogprobsOut& out, const elem_t<
   }
 }
 
-// The waves of a workgroup join theirs in a tree; wave 0 has the result.  Ends with LDS free for the next turn.
-template <int WAVES, bool TOP>
-__device__ __forceinline__ void join_waves(RowSums& a, TopKey& best, RowSums* lds_sums, TopKey (*lds_keys)[128], int wave, int lane) {
+// The sums of up to 16 waves, one from each of the first lanes.
+template <int WAVES>
+__device__ __forceinline__ RowSums join_sums(const RowSums* lds_sums, int lane) {
+  RowSums a = lane < WAVES ? lds_sums[lane] : RowSums{kLowest, 0.0f, 0.0f, 0.0f};
+  auto step = [&](auto off) {
+    constexpr int OFF = decltype(off)::value;
+    a = join(a, {lane_xor<OFF>(a.m, lane), lane_xor<OFF>(a.n, lane), lane_xor<OFF>(a.s, lane), lane_xor<OFF>(a.t, lane)});
+  };
+  using std::integral_constant;
+  if constexpr (WAVES > 1) step(integral_constant<int, 1>{});
+  if constexpr (WAVES > 2) step(integral_constant<int, 2>{});
+  if constexpr (WAVES > 4) step(integral_constant<int, 7>{});
+  if constexpr (WAVES > 8) step(integral_constant<int, 15>{});
+  auto first = [](float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); };
+  return {first(a.m), first(a.n), first(a.s), first(a.t)};
+}
+// The best of all waves' descending lists by merges in a tree; wave 0 has the result.
+template <int WAVES, typename K, int N>
+__device__ __forceinline__ K join_best(K best, K (*lds_keys)[N], int wave, int lane) {
 #pragma unroll
   for (int half = WAVES / 2; half; half /= 2) {
-    if (wave >= half && wave < 2 * half) {
-      if (lane == 0) lds_sums[wave] = a;
-      if constexpr (TOP) lds_keys[wave][lane] = best;
-    }
+    if (wave >= half && wave < 2 * half) lds_keys[wave][lane] = best;
     __syncthreads();
-    if (wave < half) {
-      a = join(a, lds_sums[wave + half]);
-      if constexpr (TOP) best = merge_lanes(best, lds_keys[wave + half][lane], lane);
+    if (wave < half) best = merge_lanes(best, lds_keys[wave + half][lane], lane);
+  }
+  return best;
+}
+
+// Where a lane's u-th group of a tile begins.  The groups that reach past the end of a row (or part) lie on its last V
+// elements instead, if it has V; what other groups hold of them counts as -inf.
+template <Elem E>
+__device__ __forceinline__ int64_t group_start(int64_t tile, int u, int64_t end, int lane) {
+  return min(tile + (u * 64 + lane) * kWordsElems<E>, max(end - kWordsElems<E>, (int64_t)0));
+}
+template <Elem E>
+__device__ __forceinline__ void load_tile(Words (&raw)[kLogpUnroll], const elem_t<E>* x_row, int64_t tile, int64_t end, int lane, bool once) {
+  constexpr int V = kWordsElems<E>, U = kLogpUnroll;
+  if (tile + 64 * V * U <= end) {
+    const elem_t<E>* p = x_row + tile + lane * V;
+    if (once) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) raw[u] = load_words<E>(p + u * 64 * V, true);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) raw[u] = load_words<E>(p + u * 64 * V, false);
     }
+  } else if (end >= V) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t j = group_start<E>(tile, u, end, lane);
+      raw[u] = without_first<E>(load_words<E>(x_row + j, false), (int)min(tile + (u * 64 + lane) * V - j, (int64_t)V));
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = load_words_part<E>(x_row, u == 0 && lane == 0 ? (int)end : 0);
   }
 }
 
@@ -234,106 +326,150 @@ __device__ __forceinline__ void join_waves(RowSums& a, TopKey& best, RowSums* ld
 // wave keep their sums relative to one score, the largest that the wave has seen: it changes in every i-th tile or so,
 // and the other tiles take no scaling.
 template <Elem E, int WAVES, bool TOP, bool ENTROPY>
-__global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void logprobs_kernel(int64_t rows, int64_t classes, const elem_t<E>* __restrict__ scores,
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void logprobs_kernel(int64_t rows, int64_t classes, const elem_t<E>* __restrict__ scores,
                                                                 int64_t row_stride, const int32_t* __restrict__ labels, int top,
-                                                                int parts, int64_t part_classes, LogprobsOut out,
+                                                                int parts, int64_t part_classes, bool once, LogprobsOut out,
                                                                 RowSums* __restrict__ part_sums, TopKey* __restrict__ part_keys) {
-  constexpr int V = kLogpVec<E>, U = kLogpUnroll, kWaves = WAVES > 4 ? WAVES : 4, kTile = 64 * V * U;
-  __shared__ TopKey lists[TOP ? kWaves : 1][128];
+  constexpr int V = kWordsElems<E>, U = kLogpUnroll, kWaves = WAVES == 1 ? 4 : WAVES, kTile = 64 * V * U;
+  __shared__ TopKey lists[TOP ? kWaves : 1][kWaiting];
+  __shared__ float segment_max[TOP ? kWaves : 1][kSegments][64];
   __shared__ RowSums wave_sums[kWaves];
+  __shared__ float lane_lists[TOP && WAVES > 1 ? kWaves : 1][64];
+  __shared__ uint16_t owners[TOP ? kWaves : 1][kWaiting];
+  __shared__ float bars[kWaves];
+  __shared__ int waiting;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part_wave = wave % WAVES;
   constexpr int kPartsPerGroup = kWaves / WAVES;
   const int64_t n_parts = rows * parts;
   for (int64_t group = blockIdx.x; group * kPartsPerGroup < n_parts; group += gridDim.x) {
     const int64_t id = group * kPartsPerGroup + wave / WAVES;
-    RowSums a{kLowest, 0.0f, 0.0f, 0.0f};
-    TopList list;
-    if constexpr (TOP) list.start(lists[wave]);
+    if (WAVES == 1 && id >= n_parts) break;
     const int64_t row = parts == 1 ? id : id / parts;
-    if (id < n_parts) {
-      const int64_t begin = parts == 1 ? 0 : (id - row * parts) * part_classes;
-      const int64_t end = min(classes, begin + part_classes);
-      const elem_t<E>* x_row = scores + row * row_stride;
-      bool first = true;
-      for (int64_t tile = begin + (int64_t)part_wave * kTile; tile < end; tile += (int64_t)WAVES * kTile) {
-        Pack<E, V> raw[U];
-        if (tile + kTile <= end) {
+    const int64_t begin = parts == 1 ? 0 : (id - row * parts) * part_classes;
+    const int64_t end = min(classes, begin + part_classes);
+    const elem_t<E>* x_row = scores + row * row_stride;
+    RowSums a{kLowest, 0.0f, 0.0f, 0.0f};
+    int32_t wanted = -1;  // asked for here, waited for behind the row's own loads
+    if (parts == 1 && part_wave == 0 && out.logprob) wanted = labels[row];
+    constexpr int64_t kStep = (int64_t)WAVES * kTile;
+    const int64_t first = begin + (int64_t)part_wave * kTile;
+    const int segment_tiles = (int)((end - begin + kStep * kSegments - 1) / (kStep * kSegments));
+    float c = reference(a.m), seen_max = -INFINITY, lane_best = -INFINITY;
+    int segment = 0, in_segment = 0;
+    float n = 0.0f;  // scores equal to a.m in the whole wave
+    for (int64_t tile = first; tile < end; tile += kStep) {
+      Words raw[U];
+      load_tile<E>(raw, x_row, tile, end, lane, once);
+      float lane_max = word_elem<E>(raw[0], 0);
 #pragma unroll
-          for (int u = 0; u < U; ++u) raw[u] = stream_pack<E, V>(x_row + tile + (u * 64 + lane) * V);
-        } else {
+      for (int k = 1; k < U * V; ++k) lane_max = __builtin_elementwise_maximum(lane_max, word_elem<E>(raw[k / V], k % V));
+      if (__ballot(!(lane_max < a.m)) == 0) {
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const int64_t j = tile + (u * 64 + lane) * V;
-            if (j + V <= end)
-              raw[u] = load_pack<E, V>(x_row + j);
-            else
-              raw[u] = load_part<E, V>(x_row + j, (int)max((int64_t)0, end - j), -INFINITY);
-          }
+        for (int k = 0; k < U * V; ++k) {
+          const float d = fmaxf(__builtin_fmaf(word_elem<E>(raw[k / V], k % V), kLog2e, -c), kFarBelow), e = __builtin_amdgcn_exp2f(d);
+          a.s += e;
+          if constexpr (ENTROPY) a.t += d * e;
         }
-        float group_max[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          group_max[u] = (float)raw[u].v[0];
-#pragma unroll
-          for (int i = 1; i < V; ++i) group_max[u] = __builtin_elementwise_maximum(group_max[u], (float)raw[u].v[i]);
+      } else {
+        const float m = reduce_lanes(__builtin_elementwise_maximum(lane_max, a.m), lane, [](float x, float y) { return __builtin_elementwise_maximum(x, y); });
+        if (!(m == a.m)) {
+          a.n = lane == 0 ? n : 0.0f;
+          a = raised(a, m);
+          c = reference(m);
+          n = 0.0f;
         }
-        float lane_max = group_max[0];
+        int equal = 0;
 #pragma unroll
-        for (int u = 1; u < U; ++u) lane_max = __builtin_elementwise_maximum(lane_max, group_max[u]);
-        if (__ballot(!(lane_max < a.m)) == 0) {
-#pragma unroll
-          for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-              const float d = fmaxf((float)raw[u].v[i] - a.m, kFarBelow), e = exp_fast(d);
-              a.s += e;
-              if constexpr (ENTROPY) a.t += d * e;
-            }
-        } else {
-          const float m = reduce_lanes(__builtin_elementwise_maximum(lane_max, a.m), lane, [](float x, float y) { return __builtin_elementwise_maximum(x, y); });
-          if (!(m == a.m)) a = raised(a, m);
-#pragma unroll
-          for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-              const float x = (float)raw[u].v[i], d = fmaxf(x - m, kFarBelow), e = exp_fast(d);
-              a.n += x == m ? 1.0f : 0.0f;
-              a.s += x == m ? 0.0f : e;
-              if constexpr (ENTROPY) a.t += d * e;
-            }
+        for (int k = 0; k < U * V; ++k) {
+          float x = word_elem<E>(raw[k / V], k % V);
+          equal += __popcll(__ballot(x == m));
+          x = x == m ? -INFINITY : x;
+          const float d = fmaxf(__builtin_fmaf(x, kLog2e, -c), kFarBelow), e = __builtin_amdgcn_exp2f(d);
+          a.s += e;
+          if constexpr (ENTROPY) a.t += d * e;
         }
-        if constexpr (TOP) {
-          if (first) list.guess(lane_max, lane, top);
-          first = false;
-          if (__ballot(lane_max >= list.score)) {
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-              if (__ballot(group_max[u] >= list.score))
-#pragma unroll
-                for (int i = 0; i < V; ++i) list.offer((float)raw[u].v[i], (int32_t)(tile + (u * 64 + lane) * V + i), lane, top);
-          }
+        n += (float)equal;
+      }
+      if constexpr (TOP) {
+        lane_best = fmaxf(lane_best, lane_max);
+        seen_max = fmaxf(seen_max, lane_max);
+        if (++in_segment == segment_tiles || tile + kStep >= end) {
+          segment_max[wave][segment++][lane] = seen_max;
+          seen_max = -INFINITY;
+          in_segment = 0;
         }
       }
     }
+    const Label label = label_at<E>(wanted, x_row, classes);
     auto add = [](float x, float y) { return x + y; };
-    a.n = reduce_lanes(a.n, lane, add);
+    a.n = n;
     a.s = reduce_lanes(a.s, lane, add);
     if constexpr (ENTROPY) a.t = reduce_lanes(a.t, lane, add);
-    if constexpr (TOP) list.take(lane, top);
     if constexpr (WAVES > 1) {
-      static_assert(WAVES == kWaves, "one part per workgroup");
-      join_waves<WAVES, TOP>(a, list.best, wave_sums, lists, wave, lane);
+      if (lane == 0) wave_sums[wave] = a;
+      if (wave == 0 && lane == 0) waiting = 0;
+      if constexpr (!TOP) __syncthreads();
     }
-    if (part_wave == 0 && id < n_parts) {
+    TopList list;
+    if constexpr (TOP) {
+      float bar = sort_lanes(lane_best, lane, 64);
+      if (WAVES > 1 && top > 8) bar = join_best<WAVES>(bar, lane_lists, wave, lane);
+      bar = fmaxf(__shfl(bar, top - 1), kLowest);  // never -inf: a masked class, or what lies behind the row
+      if constexpr (WAVES > 1) {
+        // the bar of all lanes, or for few classes the highest of the waves': with less waiting, if a little lower
+        if (lane == 0) bars[wave] = bar;
+        __syncthreads();
+        bar = bars[0];
+        if (top <= 8)
+          for (int w = 1; w < WAVES; ++w) bar = fmaxf(bar, bars[w]);
+      }
+      auto look = [&](auto&& least, auto&& see) {
+        look_again<E>(x_row, segment_max[wave], owners[wave], segment, segment_tiles, first, kStep, end, lane, least, see);
+      };
+      auto alone = [&] {  // every wave keeps its own best, whatever comes
+        list.start(lists[wave], bar);
+        look([&] { return list.score; }, [&](float x, int32_t j) { list.offer(x, j, lane, top); });
+        list.take(lane, top);
+      };
+      if constexpr (WAVES == 1) {
+        alone();
+      } else {
+        // all waves into one list, which nearly always takes it
+        TopKey* all = lists[0];
+        look([&] { return bar; }, [&](float x, int32_t j) {
+          const uint64_t hits = __ballot(x >= bar);
+          if (hits == 0) return;
+          int at = 0;
+          if (lane == 0) at = __hip_atomic_fetch_add(&waiting, __popcll(hits), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+          at = __builtin_amdgcn_readfirstlane(at) + lanes_below(hits);
+          if (x >= bar && at < kWaiting) all[at] = top_key(x, j);
+        });
+        __syncthreads();
+        const int n = waiting;
+        if (n <= kWaiting) {
+          if (wave == 0) {
+            list.best = sort_lanes(lane < n ? all[lane] : (TopKey)0, lane, n);
+            if (n > 64) list.best = merge_lanes(list.best, sort_lanes(lane < n - 64 ? all[64 + lane] : (TopKey)0, lane, n - 64), lane);
+          }
+        } else {
+          __syncthreads();  // all have read `waiting`
+          alone();
+          list.best = join_best<WAVES>(list.best, lists, wave, lane);
+        }
+      }
+    }
+    if constexpr (WAVES > 1)
+      if (wave == 0) a = join_sums<WAVES>(wave_sums, lane);
+    if (part_wave == 0) {
       if (parts == 1) {
-        finish_row<E>(out, scores, row_stride, classes, labels, row, a, TOP ? list.best : 0, top, lane);
+        finish_row<E>(out, row, label, a, TOP ? list.best : 0, top, lane);
       } else {
         if (lane == 0) part_sums[id] = a;
         if constexpr (TOP)
           if (lane < top) part_keys[id * top + lane] = list.best;
       }
     }
-    if constexpr (WAVES > 1) __syncthreads();  // wave 0 has read the last list
+    if constexpr (WAVES > 1) __syncthreads();  // LDS is free for the next part
   }
 }
 
@@ -343,18 +479,22 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(int64_t rows, int64_
                                                            int64_t row_stride, const int32_t* __restrict__ labels, int top, int parts,
                                                            LogprobsOut out, const RowSums* __restrict__ part_sums,
                                                            const TopKey* __restrict__ part_keys) {
-  __shared__ TopKey lists[4][128];
+  __shared__ TopKey lists[4][kWaiting];
   __shared__ RowSums wave_sums[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
     RowSums a{kLowest, 0.0f, 0.0f, 0.0f};
     TopKey best = 0;
+    const int32_t wanted = out.logprob ? labels[row] : -1;
     for (int p = wave; p < parts; p += 4) {
       a = join(a, part_sums[row * parts + p]);
       if (top) best = merge_lanes(best, lane < top ? part_keys[(row * parts + p) * top + lane] : (TopKey)0, lane);
     }
-    join_waves<4, true>(a, best, wave_sums, lists, wave, lane);
-    if (wave == 0) finish_row<E>(out, scores, row_stride, classes, labels, row, a, best, top, lane);
+    const Label label = label_at<E>(wanted, scores + row * row_stride, classes);
+    if (lane == 0) wave_sums[wave] = a;
+    best = join_best<4>(best, lists, wave, lane);  // its barriers are the sums' too
+    a = join_sums<4>(wave_sums, lane);
+    if (wave == 0) finish_row<E>(out, row, label, a, best, top, lane);
     __syncthreads();
   }
 }
@@ -369,7 +509,7 @@ __global__ __launch_bounds__(kGradThreads) void logprobs_grad_kernel(int64_t row
                                                                      const float* __restrict__ dlogprob,
                                                                      const float* __restrict__ dentropy, int across_shift,
                                                                      int64_t chunks, elem_t<E>* out, int64_t out_stride) {
-  constexpr int V = kLogpVec<E>;
+  constexpr int V = kWordsElems<E>;
   const int across = 1 << across_shift, down = kGradThreads >> across_shift;
   const int64_t turns = (rows + down - 1) / down * chunks;
   for (int64_t turn = blockIdx.x; turn < turns; turn += gridDim.x) {

@@ -17,6 +17,8 @@ using namespace swconv;
 namespace {
 
 constexpr int64_t kMost = (int64_t)1 << 40;  // elements between a tensor's first and last one
+// What a pass may read and leave in the 256 MB cache for the next one (a gradient reads its scores again).
+constexpr int64_t kCacheBytes = (int64_t)192 << 20;
 constexpr int64_t kMaxGroups = (int64_t)1 << 20;  // workgroups of a launch; more work is done in turns
 
 // The stream's device while a call launches, if that is not the current one.
@@ -153,20 +155,28 @@ int check_scores(int dtype, int64_t rows, int64_t classes, int64_t given, int64_
   return rows > kMost || *stride > kMost || (rows > 1 && rows - 1 > kMost / *stride) ? SWCONV_EUNSUPPORTED : SWCONV_OK;
 }
 
+// How many waves share a row, and into how many parts it is cut.  A tile is what a wave reads at a time (8 KB of fp32, 4 of
+// the 16-bit types).  Times of bf16 rows with the best 5, in us:
+//   a wave per row where rows alone fill the chip (1024 SIMDs) and are short enough for their number: 2048 x 20000 30
+//   (four waves 39), 1024 x 131072 92 (71); past 8 tiles for up to 8 best classes only (4096 x 131072 with the best 20: 243, four
+//   waves 216, whose bar is that of more lanes); and rows of one or two tiles in any case;
+//   four waves of a workgroup, sixteen for long rows that leave CUs idle: 256 x 131072 24 (four waves 31);
+//   parts of at least 6 tiles and a second launch for few rows, up to two workgroups a CU: 1 x 131072 13 (one workgroup 18.5),
+//   64 x 131072 17 (21); from 64 rows on parts of 16 tiles, past 128 rows none: 256 x 131072 in two parts 35 (24).
 struct Parts {
   int waves, parts;
   int64_t part_classes;
 };
-Parts parts_of(int dtype, int64_t rows, int64_t classes) {
-  const int64_t tile = 64 * (16 / size_of(dtype)) * kLogpUnroll;
-  if (classes <= 2 * tile) return {1, 1, classes};
-  if (rows > 256) return {4, 1, classes};
-  if (classes <= 32 * tile) return {16, 1, classes};
-  int64_t parts = std::clamp<int64_t>(512 / std::max<int64_t>(rows, 1), 1, std::max<int64_t>(1, classes / (16 * tile)));
-  parts = std::min<int64_t>(parts, 64);
-  int64_t part = (classes + parts - 1) / parts;
-  part = (part + tile - 1) / tile * tile;
-  return {16, (int)((classes + part - 1) / part), part};
+Parts parts_of(int dtype, int64_t rows, int64_t classes, int top) {
+  const int64_t tile = 64 * (16 / size_of(dtype)) * kLogpUnroll, tiles = (classes + tile - 1) / tile;
+  if (tiles <= 2 || (rows >= 1024 && tiles * 96 <= rows && (tiles <= 8 || top <= 8))) return {1, 1, classes};
+  if (rows > 256 || tiles < 12) return {4, 1, classes};
+  int64_t parts = 1;
+  if (rows > 0 && rows <= 128)
+    parts = std::min({(int64_t)512 / rows, tiles / (rows >= 64 ? 16 : 6), 16 + tiles / 64, (int64_t)64});
+  if (parts < 3) return {16, 1, classes};
+  const int64_t each = ((tiles + parts - 1) / parts + 3) / 4 * 4 * tile;  // as many tiles to each of its four waves
+  return {4, (int)((classes + each - 1) / each), each};
 }
 int64_t parts_bytes(const Parts& p, int64_t rows, int top) {
   return p.parts == 1 ? 0 : rows * p.parts * ((int64_t)sizeof(RowSums) + top * (int64_t)sizeof(TopKey));
@@ -264,7 +274,7 @@ int swconv_logprobs_workspace_bytes(int dtype, int64_t rows, int64_t classes, in
   if (int rc = check_scores(dtype, rows, classes, 0, &stride)) return rc;
   if (top < 0) return SWCONV_EINVAL;
   if (top > kTopMax) return SWCONV_EUNSUPPORTED;
-  *bytes = parts_bytes(parts_of(dtype, rows, classes), rows, top);
+  *bytes = parts_bytes(parts_of(dtype, rows, classes, top), rows, top);
   return SWCONV_OK;
 }
 
@@ -282,23 +292,24 @@ int swconv_logprobs_forward(int dtype, int64_t rows, int64_t classes, const void
   for (const void* p : {(const void*)labels_dev, (const void*)logprob_dev, (const void*)entropy_dev, (const void*)stats_dev,
                         (const void*)top_class_dev, (const void*)top_logprob_dev})
     if ((uintptr_t)p % 4) return SWCONV_EINVAL;
-  const Parts pt = parts_of(dtype, rows, classes);
+  const Parts pt = parts_of(dtype, rows, classes, top);
   if (pt.parts > 1 && (!workspace_dev || (uintptr_t)workspace_dev % 16 || workspace_bytes < parts_bytes(pt, rows, top))) return SWCONV_EINVAL;
   auto* part_sums = (RowSums*)workspace_dev;
   auto* part_keys = (TopKey*)(part_sums + rows * pt.parts);
   const LogprobsOut out{logprob_dev, entropy_dev, stats_dev, top_class_dev, top_logprob_dev};
   const hipStream_t st = (hipStream_t)hip_stream;
   const StreamDevice device(st);
+  const bool once = rows * classes * size_of(dtype) > kCacheBytes;
   return dispatch_type(dtype, [&](auto e) {
     constexpr Elem E = decltype(e)::value;
     const auto* s = (const elem_t<E>*)scores_dev;
     auto part = [&](auto waves, auto with_top, auto with_entropy) {
       constexpr int W = decltype(waves)::value;
-      constexpr int kRows = W < 4 ? 4 / W : 1;  // parts of a workgroup
+      constexpr int kRows = W == 1 ? 4 : 1;  // parts of a workgroup
       const int64_t groups = (rows * pt.parts + kRows - 1) / kRows;
       return launch(logprobs_kernel<E, W, decltype(with_top)::value, decltype(with_entropy)::value>,
-                    dim3((unsigned)std::min(groups, kMaxGroups)), W < 4 ? 256 : W * 64, st, rows, classes, s, row_stride, labels_dev, top, pt.parts,
-                    pt.part_classes, out, part_sums, part_keys);
+                    dim3((unsigned)std::min(groups, kMaxGroups)), W == 1 ? 256 : W * 64, st, rows, classes, s, row_stride, labels_dev, top, pt.parts,
+                    pt.part_classes, once, out, part_sums, part_keys);
     };
     auto entropy = [&](auto waves, auto with_top) {
       return entropy_dev ? part(waves, with_top, std::true_type{}) : part(waves, with_top, std::false_type{});
@@ -332,7 +343,7 @@ int swconv_logprobs_backward(int dtype, int64_t rows, int64_t classes, const voi
   const StreamDevice device(st);
   return dispatch_type(dtype, [&](auto e) {
     constexpr Elem E = decltype(e)::value;
-    constexpr int V = kLogpVec<E>;
+    constexpr int V = kWordsElems<E>;
     const int64_t groups = (classes + V - 1) / V;
     const int shift = std::min(8, ceil_log2(groups));
     const int64_t chunks = (groups + (1 << shift) - 1) >> shift, down = kGradThreads >> shift;
