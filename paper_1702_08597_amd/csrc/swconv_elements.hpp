@@ -58,6 +58,14 @@ __device__ __forceinline__ Words load_words(const elem_t<E>* p, bool once) {
   return once ? (Words)__builtin_nontemporal_load(q) : (Words)*q;
 }
 template <Elem E>
+__device__ __forceinline__ void store_words(elem_t<E>* p, const Words& w, bool once) {
+  auto* q = reinterpret_cast<LooseWords*>(p);
+  if (once)
+    __builtin_nontemporal_store((LooseWords)w, q);
+  else
+    *q = w;
+}
+template <Elem E>
 constexpr uint32_t kMinusInf = E == Elem::f32 ? 0xff800000u : E == Elem::bf16 ? 0xff80u : 0xfc00u;
 // The first n elements of a row that is shorter than 16 bytes, -inf behind them.
 template <Elem E>

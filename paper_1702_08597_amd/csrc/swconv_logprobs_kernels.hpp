@@ -500,48 +500,121 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(int64_t rows, int64_
 }
 
 // ---- backward ---------------------------------------------------------------------------------------------------
-// `across` threads (a power of two) share a row or, of a long row, a chunk; a thread takes one 16-byte group.
-constexpr int kGradThreads = 256;
-template <Elem E>
-__global__ __launch_bounds__(kGradThreads) void logprobs_grad_kernel(int64_t rows, int64_t classes, const elem_t<E>* scores,
-                                                                     int64_t row_stride, const int32_t* __restrict__ labels,
-                                                                     const float* __restrict__ stats, const float* __restrict__ entropy,
-                                                                     const float* __restrict__ dlogprob,
-                                                                     const float* __restrict__ dentropy, int across_shift,
-                                                                     int64_t chunks, elem_t<E>* out, int64_t out_stride) {
+// With e = exp(x - m) and p = e exp(-ls):  d x = -p (g + h (x - m - ls + H)) = e (b + a log2 e), a and b by row.  The
+// exponent holds x - m alone: ls in it would cost the digits of its size.
+struct GradRow {
+  float m, a, b, g;
+  int32_t label;
+  bool plain;  // all of them are finite
+};
+struct GradIn {
+  const int32_t* labels;
+  const float *stats, *entropy, *dlogprob, *dentropy;
+};
+__device__ __forceinline__ GradRow grad_row(const GradIn& in, int64_t row, int64_t classes) {
+  GradRow r;
+  r.m = in.stats[2 * row];
+  const float ls = in.stats[2 * row + 1];
+  r.label = in.labels ? in.labels[row] : -1;
+  const float g = in.dlogprob ? in.dlogprob[row] : 0.0f;
+  r.g = !in.dlogprob || r.label < 0 ? 0.0f : r.label < classes ? g : NAN;
+  const float h = in.dentropy ? in.dentropy[row] : 0.0f, H = in.dentropy ? in.entropy[row] : 0.0f;
+  const float scale = -__builtin_amdgcn_exp2f(-ls * kLog2e);
+  r.a = scale * h * kLn2;
+  r.b = scale * (r.g + h * (H - ls));
+  r.plain = fabsf(r.m) < INFINITY && fabsf(r.a) < INFINITY && fabsf(r.b) < INFINITY;
+  return r;
+}
+// 16 bytes of scores that begin with class j into 16 bytes of gradients.
+template <Elem E, bool ENTROPY>
+__device__ __forceinline__ Words grad_words(const GradRow& r, const Words& x, int64_t j) {
   constexpr int V = kWordsElems<E>;
-  const int across = 1 << across_shift, down = kGradThreads >> across_shift;
-  const int64_t turns = (rows + down - 1) / down * chunks;
-  for (int64_t turn = blockIdx.x; turn < turns; turn += gridDim.x) {
-    const int64_t row0 = chunks == 1 ? turn : turn / chunks;
-    const int64_t row = row0 * down + (threadIdx.x >> across_shift);
-    const int64_t j = ((turn - row0 * chunks) * across + (threadIdx.x & (across - 1))) * V;
-    if (row >= rows || j >= classes) continue;
-    const float m = stats[2 * row], ls = stats[2 * row + 1];
-    const int32_t label = labels ? labels[row] : -1;
-    float g = 0.0f;
-    if (dlogprob && label >= 0) g = label < classes ? dlogprob[row] : NAN;
-    const float h = dentropy ? dentropy[row] : 0.0f, H = dentropy ? entropy[row] : 0.0f;
-    const bool empty = m == -INFINITY;
-    const elem_t<E>* x_row = scores + row * row_stride + j;
-    const int n = (int)min((int64_t)V, classes - j);
-    const Pack<E, V> x = n == V ? load_pack<E, V>(x_row) : load_part<E, V>(x_row, n, -INFINITY);
-    Pack<E, V> dx;
+  Pack<E, V> out;
+  const int64_t hot = r.label - j;
+  if (r.plain) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const float xi = (float)x.v[i];
-      const float lp = fmaxf(xi - m, kFarBelow) - ls;  // far below p is 0
-      const float p = exp_fast(lp);
-      float d = -p * (g + h * (lp + H));
-      if (j + i == label) d += g;
-      if (m != m) d = NAN;
-      dx.v[i] = (elem_t<E>)(empty || xi == -INFINITY ? 0.0f : d);
+      float d = (word_elem<E>(x, i) - r.m) * kLog2e;
+      if constexpr (ENTROPY) d = fmaxf(d, kFarBelow);
+      const float e = __builtin_amdgcn_exp2f(d);
+      out.v[i] = (elem_t<E>)(e * (ENTROPY ? __builtin_fmaf(r.a, d, r.b) : r.b));
     }
-    if (n == V)
-      store_pack<E, V>(out + row * out_stride + j, dx);
-    else
-      store_part<E, V>(out + row * out_stride + j, n, dx);
+    if (hot >= 0 && hot < V)
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (hot == i) {
+          const float xi = word_elem<E>(x, i), d = fmaxf((xi - r.m) * kLog2e, kFarBelow);
+          out.v[i] = (elem_t<E>)(xi > -INFINITY ? r.g + __builtin_amdgcn_exp2f(d) * __builtin_fmaf(r.a, d, r.b) : 0.0f);
+        }
+  } else {
+    // no class left (all 0), a row of NaN, or a gradient that is not finite; masked classes get 0 here too
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float xi = word_elem<E>(x, i), d = fmaxf((xi - r.m) * kLog2e, kFarBelow);
+      float v = r.m != r.m ? NAN : __builtin_amdgcn_exp2f(d) * (r.a * d + r.b);
+      if (hot == i) v += r.g;
+      out.v[i] = (elem_t<E>)(xi == -INFINITY ? 0.0f : v);
+    }
   }
+  return __builtin_bit_cast(Words, out);
+}
+template <Elem E, bool ENTROPY>
+__device__ __forceinline__ void grad_group(const GradRow& r, const elem_t<E>* x_row, elem_t<E>* out_row, int64_t j, int64_t classes) {
+  constexpr int V = kWordsElems<E>;
+  if (j + V <= classes) {
+    store_words<E>(out_row + j, grad_words<E, ENTROPY>(r, load_words<E>(x_row + j, false), j), false);
+  } else if (j < classes) {
+    const int n = (int)(classes - j);
+    const Pack<E, V> dx = __builtin_bit_cast(Pack<E, V>, grad_words<E, ENTROPY>(r, load_words_part<E>(x_row + j, n), j));
+    store_part<E, V>(out_row + j, n, dx);
+  }
+}
+
+// Rows of at least 128 groups of 16 bytes: workgroups along a row, in the order of memory; the row's numbers are scalars
+// and arrive with the scores.  Groups to a thread: 4096 x 131072 bf16 with one 446 us, two 354, four 368; 4096 x 65536 f32
+// 337, 362, 361.
+constexpr int kGradThreads = 256;
+template <Elem E>
+constexpr int kGradUnroll = E == Elem::f32 ? 1 : 2;
+template <Elem E, bool ENTROPY>
+__global__ __launch_bounds__(kGradThreads) void logprobs_grad_kernel(int64_t rows, int64_t classes, const elem_t<E>* scores, int64_t row_stride,
+                                                                     GradIn in, bool once, elem_t<E>* out, int64_t out_stride) {
+  constexpr int V = kWordsElems<E>, U = kGradUnroll<E>;
+  const int64_t j = ((int64_t)blockIdx.x * (kGradThreads * U) + threadIdx.x) * V;
+  for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+    const elem_t<E>* x_row = scores + row * row_stride;
+    elem_t<E>* out_row = out + row * out_stride;
+    if (((int64_t)blockIdx.x + 1) * (kGradThreads * U) * V <= classes) {
+      Words x[U];
+      if (once) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = load_words<E>(x_row + j + u * (kGradThreads * V), true);
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = load_words<E>(x_row + j + u * (kGradThreads * V), false);
+      }
+      const GradRow r = grad_row(in, row, classes);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t at = j + u * (kGradThreads * V);
+        store_words<E>(out_row + at, grad_words<E, ENTROPY>(r, x[u], at), once);
+      }
+    } else {
+      const GradRow r = grad_row(in, row, classes);
+#pragma unroll
+      for (int u = 0; u < U; ++u) grad_group<E, ENTROPY>(r, x_row, out_row, j + u * (kGradThreads * V), classes);
+    }
+  }
+}
+// Shorter rows: `across` threads (a power of two) to a row.
+template <Elem E, bool ENTROPY>
+__global__ __launch_bounds__(kGradThreads) void logprobs_grad_short_kernel(int64_t rows, int64_t classes, const elem_t<E>* scores,
+                                                                           int64_t row_stride, GradIn in, int across_shift,
+                                                                           elem_t<E>* out, int64_t out_stride) {
+  const int across = 1 << across_shift, down = kGradThreads >> across_shift;
+  const int64_t j = (threadIdx.x & (across - 1)) * kWordsElems<E>;
+  for (int64_t row = (int64_t)blockIdx.x * down + (threadIdx.x >> across_shift); row < rows; row += (int64_t)gridDim.x * down)
+    grad_group<E, ENTROPY>(grad_row(in, row, classes), scores + row * row_stride, out + row * out_stride, j, classes);
 }
 
 }  // namespace swconv

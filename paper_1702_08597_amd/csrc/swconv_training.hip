@@ -341,16 +341,24 @@ int swconv_logprobs_backward(int dtype, int64_t rows, int64_t classes, const voi
     if ((uintptr_t)p % 4) return SWCONV_EINVAL;
   const hipStream_t st = (hipStream_t)hip_stream;
   const StreamDevice device(st);
+  const GradIn in{labels_dev, stats_dev, entropy_dev, dlogprob_dev, dentropy_dev};
+  const bool once = 2 * rows * classes * size > kCacheBytes;
   return dispatch_type(dtype, [&](auto e) {
     constexpr Elem E = decltype(e)::value;
-    constexpr int V = kWordsElems<E>;
-    const int64_t groups = (classes + V - 1) / V;
-    const int shift = std::min(8, ceil_log2(groups));
-    const int64_t chunks = (groups + (1 << shift) - 1) >> shift, down = kGradThreads >> shift;
-    const int64_t turns = (rows + down - 1) / down * chunks;
-    return launch(logprobs_grad_kernel<E>, dim3((unsigned)std::min(turns, kMaxGroups)), kGradThreads, st, rows, classes,
-                  (const elem_t<E>*)scores_dev, row_stride, labels_dev, stats_dev, entropy_dev, dlogprob_dev, dentropy_dev, shift, chunks,
-                  (elem_t<E>*)dscores_dev, dscores_stride);
+    const auto* s = (const elem_t<E>*)scores_dev;
+    auto* d = (elem_t<E>*)dscores_dev;
+    const int64_t groups = (classes + kWordsElems<E> - 1) / kWordsElems<E>;
+    auto grad = [&](auto with_entropy) {
+      constexpr bool H = decltype(with_entropy)::value;
+      if (groups >= 128)
+        return launch(logprobs_grad_kernel<E, H>, dim3((unsigned)((groups + kGradThreads * kGradUnroll<E> - 1) / (kGradThreads * kGradUnroll<E>)), (unsigned)std::min<int64_t>(rows, 65535)),
+                      kGradThreads, st, rows, classes, s, row_stride, in, once, d, dscores_stride);
+      const int shift = ceil_log2(groups);
+      const int64_t down = kGradThreads >> shift;
+      return launch(logprobs_grad_short_kernel<E, H>, dim3((unsigned)std::min((rows + down - 1) / down, kMaxGroups)), kGradThreads, st, rows,
+                    classes, s, row_stride, in, shift, d, dscores_stride);
+    };
+    return dentropy_dev ? grad(std::true_type{}) : grad(std::false_type{});
   });
 }
 
