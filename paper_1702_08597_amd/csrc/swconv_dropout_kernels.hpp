@@ -3,16 +3,18 @@
 //   dz = keep and (z > 0 or no relu) ? dy * scale : 0,  dx = dz,  dbias[k] = sum over n, s of dz
 // The mask is never stored: keep(row, col) = 16-bit field col % 8 of philox4x32-10 (Salmon, Moraes, Dror, Shaw,
 // "Parallel random numbers: as easy as 1, 2, 3", 2011) at counter {col / 8, row, step}, so that any thread makes any
-// element's decision alone and the backward pass makes the forward pass's.  A group of 8 columns costs one call, 20
+// element's decision alone and the backward pass makes the forward pass's.  An item of 8 columns costs one call, 20
 // products of 32 x 32 bits.  16 bits an element round the rate to a multiple of 2^-16; the scale is that rate's, so the
 // mean is kept exactly.  Arithmetic in fp32, one rounding to the element type at the end.
 #pragma once
 #include "swconv_elements.hpp"
+#include "swconv_lanes.hpp"
 
 namespace swconv {
 
 constexpr int kDropThreads = 256;
-constexpr int kDropItems = 2;      // groups of 8 columns per thread and turn
+template <Elem E>
+constexpr int kDropSteps = E == Elem::f32 ? 1 : 2;  // of 64 groups of 8 columns, to a wave and turn
 constexpr int kDropUnit = 512;     // groups that a wave of the gradient of maps sums up at a time
 
 struct DropoutRule {
@@ -22,150 +24,287 @@ struct DropoutRule {
   float scale;
   int relu;
 };
+struct Generator {
+  uint64_t seed, step;
+  __device__ __forceinline__ explicit Generator(const DropoutRule& rule)
+      : seed(rule.threshold ? rule.rng[0] : 0), step(rule.threshold ? rule.rng[1] + rule.offset : 0) {}
+};
 
-// Rows of the generator: planes (n, k) of S columns, or with S = 1 images of K columns.
+// Rows of the generator: planes (n, k) of S columns, or with S = 1 images (n, 0) of K columns.  An item is a group of 8
+// columns of a row.
 struct DropoutShape {
-  Divisor groups;       // of 8 columns in a row
+  Divisor groups;       // in a row
   Divisor32 groups32, channels;
   uint64_t items;       // rows * groups
   uint32_t cols;
-  int features;         // S = 1: columns are channels
+  uint32_t pad;         // columns that the last item of a row lacks
+  uint32_t stride_group, stride_row;  // 64 / kHalves items, taken apart
 };
 
-__device__ __forceinline__ void philox_round(uint32_t (&c)[4], uint32_t k0, uint32_t k1) {
-  const uint64_t a = (uint64_t)0xD2511F53u * c[0], b = (uint64_t)0xCD9E8D57u * c[2];
-  c[0] = (uint32_t)(b >> 32) ^ c[1] ^ k0;
-  c[1] = (uint32_t)b;
-  c[2] = (uint32_t)(a >> 32) ^ c[3] ^ k1;
-  c[3] = (uint32_t)a;
+// An item; `ahead` counts it from the first one of its wave's turn.
+struct Place {
+  uint32_t row, group, ahead;
+};
+// The item `ahead` (below 2^31) behind a first one.
+__device__ __forceinline__ Place place_at(const DropoutShape& sh, uint64_t first, uint32_t ahead) {
+  const uint32_t row0 = (uint32_t)sh.groups.quotient(first);
+  const uint32_t at = (uint32_t)(first - (uint64_t)row0 * sh.groups.d) + ahead, over = sh.groups32.quotient(at);
+  return {row0 + over, at - over * sh.groups32.d, ahead};
+}
+template <int STRIDE>
+__device__ __forceinline__ Place next_place(const DropoutShape& sh, Place p) {
+  p.group += sh.stride_group;
+  const uint32_t wrap = p.group >= sh.groups32.d;
+  p.group -= wrap ? sh.groups32.d : 0;
+  p.row += sh.stride_row + wrap;
+  p.ahead += STRIDE;
+  return p;
 }
 
-// The decisions for 8 columns, bit i: column 8 * group + i is kept.
-__device__ __forceinline__ uint32_t keep_bits(const DropoutRule& rule, uint64_t seed, uint64_t step, uint32_t row, uint32_t group) {
-  if (rule.threshold == 0) return 0xffu;
-  uint32_t c[4] = {group, row, (uint32_t)step, (uint32_t)(step >> 32)};
-  uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+struct KeepWords {
+  uint32_t w[4];  // 8 fields of 16 bits
+};
+__device__ __forceinline__ KeepWords keep_words(const Generator& g, uint32_t row, uint32_t group) {
+  uint32_t c[4] = {group, row, (uint32_t)g.step, (uint32_t)(g.step >> 32)};
+  uint32_t k0 = (uint32_t)g.seed, k1 = (uint32_t)(g.seed >> 32);
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
-    philox_round(c, k0, k1);
+    const uint64_t a = (uint64_t)0xD2511F53u * c[0], b = (uint64_t)0xCD9E8D57u * c[2];
+    c[0] = __builtin_amdgcn_bitop3_b32((uint32_t)(b >> 32), c[1], k0, 0x96);  // the exclusive or of all three
+    c[1] = (uint32_t)b;
+    c[2] = __builtin_amdgcn_bitop3_b32((uint32_t)(a >> 32), c[3], k1, 0x96);
+    c[3] = (uint32_t)a;
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
   }
-  uint32_t keep = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) keep |= (uint32_t)(((c[i / 2] >> (i % 2 * 16)) & 0xffffu) >= rule.threshold) << i;
-  return keep;
+  return {{c[0], c[1], c[2], c[3]}};
 }
 
-// Where a row of the generator lies in a tensor of the given image stride, and its channel.
-__device__ __forceinline__ int64_t row_offset(const DropoutShape& sh, uint32_t row, int64_t stride, uint32_t* k) {
-  if (sh.features) {
-    *k = 0;
-    return (int64_t)row * stride;
-  }
-  const uint32_t n = sh.channels.quotient(row);
-  *k = row - n * sh.channels.d;
-  return (int64_t)n * stride + (int64_t)*k * sh.cols;
-}
+// A lane works on chunks of 16 bytes, so that a wave's accesses are runs of 1 KB.  A chunk of the 16-bit types is an item.
+// Of fp32 an item is two chunks: a pair of lanes holds two items, each lane one half of both (half 0 of the even lane
+// first), makes the words of one and gets those of its half of the other from its neighbour.
+template <Elem E>
+constexpr int kChunk = kWordsElems<E>;
+template <Elem E>
+constexpr int kHalves = 8 / kChunk<E>;
 
-__device__ __forceinline__ void load_bias(const DropoutShape& sh, const float* bias, uint32_t k, uint32_t col, int n, float (&b)[8]) {
-  if (!bias) {
+template <Elem E>
+struct Chunks {
+  Place at[kHalves<E>];
+  bool in[kHalves<E>];
+};
+template <Elem E>
+__device__ __forceinline__ uint32_t lane_item(int lane) {
+  return kHalves<E> == 1 ? lane : lane / 2;
+}
+template <Elem E>
+__device__ __forceinline__ uint32_t first_column(const Place& p, int lane) {
+  return p.group * 8 + (kHalves<E> == 1 ? 0 : (lane & 1) * 4);
+}
+// The keep words of a lane's chunks: kChunk / 2 for each.
+template <Elem E>
+__device__ __forceinline__ void chunk_words(const Generator& g, const Place& first, const Place& second, int lane,
+                                            uint32_t (&w)[kHalves<E>][kChunk<E> / 2]) {
+  if constexpr (kHalves<E> == 1) {
+    const KeepWords k = keep_words(g, first.row, first.group);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) b[i] = 0.0f;
-  } else if (!sh.features) {
-    const float v = bias[k];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) b[i] = v;
+    for (int i = 0; i < 4; ++i) w[0][i] = k.w[i];
   } else {
-    const Pack<Elem::f32, 8> v = n == 8 ? load_pack<Elem::f32, 8>(bias + col) : load_part<Elem::f32, 8>(bias + col, n, 0.0f);
+    const bool odd = lane & 1;
+    const uint32_t row0 = first.row, row1 = second.row, group0 = first.group, group1 = second.group;
+    const KeepWords k = keep_words(g, odd ? row1 : row0, odd ? group1 : group0);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) b[i] = v.v[i];
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t got = lane_xor<1>(odd ? k.w[i] : k.w[2 + i], lane);
+      w[0][i] = odd ? got : k.w[i];
+      w[1][i] = odd ? k.w[2 + i] : got;
+    }
   }
 }
+template <int N>
+__device__ __forceinline__ bool kept(const uint32_t (&w)[N], int i, uint32_t threshold) {
+  return (i % 2 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu) >= threshold;
+}
 
+// A tensor of images; `gap`: elements between one and the next, `span`: from the first to behind the last.
 template <Elem E>
-__device__ __forceinline__ Pack<E, 8> load_group(const elem_t<E>* p, int n) {
-  return n == 8 ? load_pack<E, 8>(p) : load_part<E, 8>(p, n, 0.0f);
+struct Images {
+  elem_t<E>* p;
+  int64_t gap, span;
+};
+// Where a lane's chunks begin: items of 8 columns, less what the rows before lack, and the gaps between images.
+template <Elem E, int COUNT>
+__device__ __forceinline__ void chunk_offsets(const DropoutShape& sh, uint64_t first, const Place (&at)[COUNT], int64_t gap, int lane,
+                                              int64_t (&offset)[COUNT]) {
+#pragma unroll
+  for (int c = 0; c < COUNT; ++c) {
+    offset[c] = (int64_t)(first * 8) + (at[c].ahead * 8 + (kHalves<E> == 1 ? 0 : (lane & 1) * 4)) - (int64_t)((uint64_t)at[c].row * sh.pad);
+    if (gap) offset[c] += (int64_t)sh.channels.quotient(at[c].row) * gap;
+  }
+}
+// Whether 16 bytes can be read at all of a wave's chunks.  A chunk that its row does not fill is read to its end all the same
+// (what is behind a row is not used); only behind the tensor's last elements nothing is.
+template <Elem E, int COUNT>
+__device__ __forceinline__ bool readable(const DropoutShape& sh, const Images<E>& x, uint64_t first, const Place (&at)[COUNT],
+                                         const int (&n)[COUNT], int lane) {
+  int64_t offset[COUNT];
+  chunk_offsets<E>(sh, first, at, x.gap, lane, offset);
+  bool end = x.span < kChunk<E>;
+#pragma unroll
+  for (int c = 0; c < COUNT; ++c) end |= n[c] > 0 && offset[c] + kChunk<E> > x.span;
+  return __ballot(end) == 0;
+}
+// Where readable() said no, chunks are read by the element.  The way is fixed at compile time for a whole turn: where ways
+// meet behind loads, the compiler waits for them, and they would not go out together.
+enum class Read { whole, once, elements };
+template <Elem E, Read HOW, int COUNT>
+__device__ __forceinline__ void load_chunks(const Images<E>& x, const int64_t (&offset)[COUNT], const int (&n)[COUNT], Words (&w)[COUNT]) {
+#pragma unroll
+  for (int c = 0; c < COUNT; ++c) {
+    if constexpr (HOW != Read::elements)
+      w[c] = load_words<E>(x.p + (n[c] > 0 ? offset[c] : 0), HOW == Read::once);
+    else if (n[c] > 0)
+      w[c] = n[c] == kChunk<E> ? load_words<E>(x.p + offset[c], false) : load_words_part<E>(x.p + offset[c], n[c]);
+  }
+}
+template <typename F>
+__device__ __forceinline__ void choose_read(bool whole, bool once, F&& f) {
+  using std::integral_constant;
+  if (!whole)
+    f(integral_constant<Read, Read::elements>{});
+  else if (once)
+    f(integral_constant<Read, Read::once>{});
+  else
+    f(integral_constant<Read, Read::whole>{});
 }
 template <Elem E>
-__device__ __forceinline__ void store_group(elem_t<E>* p, int n, const Pack<E, 8>& a) {
-  if (n == 8)
-    store_pack<E, 8>(p, a);
+__device__ __forceinline__ void store_chunk(elem_t<E>* p, int n, const float (&v)[kChunk<E>], bool once) {
+  Pack<E, kChunk<E>> a;
+#pragma unroll
+  for (int i = 0; i < kChunk<E>; ++i) a.v[i] = (elem_t<E>)v[i];
+  if (n >= kChunk<E>)
+    store_words<E>(p, __builtin_bit_cast(Words, a), once);
   else
-    store_part<E, 8>(p, n, a);
+    store_part<E, kChunk<E>>(p, n, a);
+}
+// Columns of a chunk that its row has (0 or less: none).
+template <Elem E>
+__device__ __forceinline__ int chunk_size(const DropoutShape& sh, uint32_t col) {
+  return (int)min((int64_t)sh.cols - col, (int64_t)kChunk<E>);
+}
+// The bias by channels of maps, by columns of features, by columns that fill no item at the end of a row.  None: zeros.
+enum class Bias { planes, columns, ragged };
+__device__ const float kNoBias[8] = {};
+struct BiasAt {
+  const float* p;
+  uint32_t step;  // 0: none
+  __device__ __forceinline__ explicit BiasAt(const float* bias) : p(bias ? bias : kNoBias), step(bias ? 1 : 0) {}
+};
+template <Elem E, Bias B>
+__device__ __forceinline__ void load_bias(const DropoutShape& sh, const BiasAt& bias, uint32_t row, uint32_t col, int n, float (&b)[kChunk<E>]) {
+  constexpr int V = kChunk<E>;
+  if constexpr (B == Bias::planes) {
+    const uint32_t k = row - sh.channels.quotient(row) * sh.channels.d;
+    const float one = bias.p[(n > 0 ? k : 0) * bias.step];
+#pragma unroll
+    for (int i = 0; i < V; ++i) b[i] = one;
+  } else if constexpr (B == Bias::columns) {
+    const Pack<Elem::f32, V> v = load_pack<Elem::f32, V>(bias.p + (n > 0 ? col : 0) * bias.step);
+#pragma unroll
+    for (int i = 0; i < V; ++i) b[i] = v.v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) b[i] = bias.p[min(col + i, sh.cols - 1) * bias.step];
+  }
 }
 
 // A dropped element is 0 whatever it was; a NaN that is kept stays one.
 template <Elem E>
-__device__ __forceinline__ Pack<E, 8> forward_group(const DropoutRule& rule, const Pack<E, 8>& x, const float (&b)[8], uint32_t keep) {
-  Pack<E, 8> y;
+__device__ __forceinline__ void forward_chunk(const DropoutRule& rule, const Words& x, const float (&b)[kChunk<E>],
+                                              const uint32_t (&w)[kChunk<E> / 2], float (&y)[kChunk<E>]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float z = (float)x.v[i] + b[i];
-    if (rule.relu && z < 0.0f) z = 0.0f;
-    y.v[i] = (elem_t<E>)(keep >> i & 1 ? z * rule.scale : 0.0f);
-  }
-  return y;
-}
-// dz of a group; the sum of its 8 in a fixed order.
-template <Elem E>
-__device__ __forceinline__ void backward_group(const DropoutRule& rule, const Pack<E, 8>& dy, const Pack<E, 8>& x, const float (&b)[8],
-                                               uint32_t keep, float (&dz)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    bool pass = keep >> i & 1;
-    if (rule.relu) pass = pass && !((float)x.v[i] + b[i] <= 0.0f);
-    dz[i] = pass ? (float)dy.v[i] * rule.scale : 0.0f;
+  for (int i = 0; i < kChunk<E>; ++i) {
+    float z = word_elem<E>(x, i) + b[i];
+    if (rule.relu) z = __builtin_elementwise_maximum(z, 0.0f);
+    y[i] = kept(w, i, rule.threshold) ? z * rule.scale : 0.0f;
   }
 }
-template <Elem E>
-__device__ __forceinline__ Pack<E, 8> rounded(const float (&v)[8]) {
-  Pack<E, 8> a;
+template <Elem E, bool RELU>
+__device__ __forceinline__ void backward_chunk(const DropoutRule& rule, const Words& dy, const Words& x, const float (&b)[kChunk<E>],
+                                               const uint32_t (&w)[kChunk<E> / 2], float (&dz)[kChunk<E>]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) a.v[i] = (elem_t<E>)v[i];
-  return a;
+  for (int i = 0; i < kChunk<E>; ++i) {
+    bool pass = kept(w, i, rule.threshold);
+    if constexpr (RELU) pass = pass && !(word_elem<E>(x, i) + b[i] <= 0.0f);
+    dz[i] = pass ? word_elem<E>(dy, i) * rule.scale : 0.0f;
+  }
 }
 
-// Forward, and backward without a bias gradient: threads over all groups of all rows.  Bound by memory: a group in
-// and a group out.
-template <Elem E, bool BACKWARD>
-__global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutShape sh, DropoutRule rule, const elem_t<E>* x,
-                                                               int64_t x_stride, const float* __restrict__ bias, const elem_t<E>* dy,
-                                                               int64_t dy_stride, elem_t<E>* out, int64_t out_stride) {
-  constexpr uint64_t kTurn = kDropThreads * kDropItems;
-  uint64_t seed = 0, step = 0;
-  if (rule.threshold) {
-    seed = rule.rng[0];
-    step = rule.rng[1] + rule.offset;
+// Forward, and backward without a bias gradient: waves over all items in the order of memory.  Bound by memory: a chunk in
+// (two with ReLU backward) and a chunk out.  GATE: the backward pass reads x for the ReLU.
+enum class Pass { forward, backward, backward_relu };
+template <Elem E, Pass PASS, Bias B, Read HOW>
+__device__ __forceinline__ void dropout_turn(const DropoutShape& sh, const DropoutRule& rule, const Images<E>& x, const float* bias,
+                                             const Images<E>& dy, const Images<E>& out, uint64_t first,
+                                             const Place (&at)[kDropSteps<E> * kHalves<E>], const int (&n)[kDropSteps<E> * kHalves<E>],
+                                             int lane) {
+  constexpr int H = kHalves<E>, V = kChunk<E>, COUNT = kDropSteps<E> * H;
+  Words in[COUNT], gate[COUNT];
+  int64_t offset[COUNT];
+  float b[COUNT][V];
+  const Images<E>& from = PASS == Pass::forward ? x : dy;
+  chunk_offsets<E>(sh, first, at, from.gap, lane, offset);
+  load_chunks<E, HOW>(from, offset, n, in);
+  if constexpr (PASS == Pass::backward_relu) {
+    if (x.gap != dy.gap) chunk_offsets<E>(sh, first, at, x.gap, lane, offset);
+    load_chunks<E, HOW>(x, offset, n, gate);
   }
-  for (uint64_t first = blockIdx.x * kTurn; first < sh.items; first += gridDim.x * kTurn) {
-    const uint64_t row0 = sh.groups.quotient(first);
-    const uint32_t group0 = (uint32_t)(first - row0 * sh.groups.d);
+  if constexpr (PASS != Pass::backward) {
+    const BiasAt by(bias);
 #pragma unroll
-    for (int u = 0; u < kDropItems; ++u) {
-      const uint32_t t = u * kDropThreads + threadIdx.x;
-      if (first + t >= sh.items) break;
-      const uint32_t over = sh.groups32.quotient(group0 + t);
-      const uint32_t row = (uint32_t)row0 + over, group = group0 + t - over * sh.groups32.d;
-      const uint32_t col = group * 8;
-      const int n = min(8u, sh.cols - col);
-      uint32_t k;
-      const int64_t o = row_offset(sh, row, out_stride, &k) + col;
-      const uint32_t keep = keep_bits(rule, seed, step, row, group);
-      float b[8];
-      load_bias(sh, bias, k, col, n, b);
-      if constexpr (!BACKWARD) {
-        const Pack<E, 8> a = load_group<E>(x + row_offset(sh, row, x_stride, &k) + col, n);
-        store_group<E>(out + o, n, forward_group<E>(rule, a, b, keep));
-      } else {
-        const Pack<E, 8> g = load_group<E>(dy + row_offset(sh, row, dy_stride, &k) + col, n);
-        Pack<E, 8> a = g;
-        if (rule.relu) a = load_group<E>(x + row_offset(sh, row, x_stride, &k) + col, n);
-        float dz[8];
-        backward_group<E>(rule, g, a, b, keep, dz);
-        store_group<E>(out + o, n, rounded<E>(dz));
-      }
+    for (int c = 0; c < COUNT; ++c) load_bias<E, B>(sh, by, at[c].row, first_column<E>(at[c], lane), n[c], b[c]);
+  }
+  const Generator g(rule);
+  if (out.gap != (PASS == Pass::backward_relu ? x.gap : from.gap)) chunk_offsets<E>(sh, first, at, out.gap, lane, offset);
+#pragma unroll
+  for (int s = 0; s < kDropSteps<E>; ++s) {
+    uint32_t w[H][V / 2] = {};
+    if (rule.threshold) chunk_words<E>(g, at[s * H], at[s * H + H - 1], lane, w);
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const int c = s * H + h;
+      float v[V];
+      if constexpr (PASS == Pass::forward)
+        forward_chunk<E>(rule, in[c], b[c], w[h], v);
+      else
+        backward_chunk<E, PASS == Pass::backward_relu>(rule, in[c], gate[c], b[c], w[h], v);
+      if (n[c] > 0) store_chunk<E>(out.p + offset[c], n[c], v, HOW == Read::once);
     }
+  }
+}
+template <Elem E, Pass PASS, Bias B>
+__global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutShape sh, DropoutRule rule, Images<E> x, const float* __restrict__ bias,
+                                                               Images<E> dy, Images<E> out, bool once) {
+  constexpr int H = kHalves<E>, COUNT = kDropSteps<E> * H;
+  const int lane = threadIdx.x & 63;
+  const uint64_t wave = (uint64_t)blockIdx.x * (kDropThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (uint64_t first = wave * (64 * kDropSteps<E>); first < sh.items; first += (uint64_t)gridDim.x * (kDropThreads * kDropSteps<E>)) {
+    const uint32_t left = (uint32_t)min(sh.items - first, (uint64_t)(64 * kDropSteps<E>));
+    Place at[COUNT];
+    int n[COUNT];
+    Place p = place_at(sh, first, lane_item<E>(lane));
+#pragma unroll
+    for (int c = 0; c < COUNT; ++c) {
+      if (c) p = next_place<64 / H>(sh, p);
+      at[c] = p;
+      n[c] = p.ahead < left ? chunk_size<E>(sh, first_column<E>(p, lane)) : 0;
+    }
+    bool whole = sh.items - first - left >= 8;  // 8 elements at least lie behind
+    if (!whole)
+      whole = (PASS == Pass::backward || readable(sh, x, first, at, n, lane)) && (PASS == Pass::forward || readable(sh, dy, first, at, n, lane));
+    choose_read(whole, once, [&](auto how) {
+      dropout_turn<E, PASS, B, decltype(how)::value>(sh, rule, x, bias, dy, out, first, at, n, lane);
+    });
   }
 }
 
@@ -179,99 +318,153 @@ struct MapUnits {
   uint32_t images;
   int planes, lane_shift; // planes per unit; lanes per plane in the final sum, as a shift
 };
-template <Elem E>
-__global__ __launch_bounds__(kDropThreads) void dropout_maps_grad_kernel(DropoutShape sh, MapUnits mu, DropoutRule rule,
-                                                                         const elem_t<E>* x, int64_t x_stride,
-                                                                         const float* __restrict__ bias, const elem_t<E>* dy,
-                                                                         int64_t dy_stride, elem_t<E>* dx, int64_t dx_stride,
-                                                                         float* __restrict__ partial) {
+template <Elem E, bool RELU>
+__global__ __launch_bounds__(kDropThreads) void dropout_maps_grad_kernel(DropoutShape sh, MapUnits mu, DropoutRule rule, Images<E> x,
+                                                                         const float* __restrict__ bias, Images<E> dy, Images<E> dx,
+                                                                         float* __restrict__ partial, bool once) {
+  constexpr int H = kHalves<E>, V = kChunk<E>;
   __shared__ float sums[kDropThreads / 64][kDropUnit];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint64_t seed = 0, step = 0;
-  if (rule.threshold) {
-    seed = rule.rng[0];
-    step = rule.rng[1] + rule.offset;
-  }
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   for (uint64_t unit = blockIdx.x * (uint64_t)(kDropThreads / 64) + wave; unit < mu.units; unit += gridDim.x * (uint64_t)(kDropThreads / 64)) {
     const uint32_t bundle = mu.segments.d == 1 ? (uint32_t)unit : (uint32_t)(unit / mu.segments.d);
     const uint32_t segment = (uint32_t)(unit - (uint64_t)bundle * mu.segments.d);
     const uint32_t row0 = bundle * mu.planes, group0 = segment * kDropUnit;
     const uint32_t planes = min((uint32_t)mu.planes, mu.rows - row0);
-    const uint32_t width = min((uint32_t)kDropUnit, sh.groups32.d - group0);
-    for (uint32_t it = lane; it < planes * width; it += 64) {
-      const uint32_t p = mu.segments.d == 1 ? sh.groups32.quotient(it) : 0;
-      const uint32_t row = row0 + p, group = group0 + it - p * width;
-      const uint32_t col = group * 8;
-      const int n = min(8u, sh.cols - col);
-      uint32_t k;
-      const Pack<E, 8> g = load_group<E>(dy + row_offset(sh, row, dy_stride, &k) + col, n);
-      Pack<E, 8> a = g;
-      if (rule.relu) a = load_group<E>(x + row_offset(sh, row, x_stride, &k) + col, n);
-      float b[8], dz[8];
-      load_bias(sh, bias, k, col, n, b);
-      backward_group<E>(rule, g, a, b, keep_bits(rule, seed, step, row, group), dz);
-      if (dx) store_group<E>(dx + row_offset(sh, row, dx_stride, &k) + col, n, rounded<E>(dz));
-      float sum = 0.0f;  // columns behind the row hold 0
+    const uint32_t width = min((uint32_t)kDropUnit, sh.groups32.d - group0), items = planes * width;
+    const uint64_t first = (uint64_t)row0 * sh.groups32.d + group0;
+    Place p = place_at(sh, first, lane_item<E>(lane));
+    for (uint32_t step = 0; step < items; step += 64) {
+      Place at[H];
+      int n[H];
+      float sum[H];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum += i < n ? dz[i] : 0.0f;
-      sums[wave][it] = sum;
+      for (int h = 0; h < H; ++h) {
+        at[h] = p;
+        p = next_place<64 / H>(sh, p);
+        n[h] = at[h].ahead < items ? chunk_size<E>(sh, first_column<E>(at[h], lane)) : 0;
+      }
+      auto turn = [&](auto how) {
+        constexpr Read HOW = decltype(how)::value;
+        Words in[H], gate[H];
+        float b[H][V];
+        int64_t offset[H];
+        chunk_offsets<E>(sh, first, at, dy.gap, lane, offset);
+        load_chunks<E, HOW>(dy, offset, n, in);
+        if constexpr (RELU) {
+          if (x.gap != dy.gap) chunk_offsets<E>(sh, first, at, x.gap, lane, offset);
+          load_chunks<E, HOW>(x, offset, n, gate);
+          const BiasAt by(bias);
+#pragma unroll
+          for (int h = 0; h < H; ++h) load_bias<E, Bias::planes>(sh, by, at[h].row, 0, n[h], b[h]);
+        }
+        const Generator g(rule);
+        uint32_t w[H][V / 2] = {};
+        if (rule.threshold) chunk_words<E>(g, at[0], at[H - 1], lane, w);
+        if (dx.gap != (RELU ? x.gap : dy.gap)) chunk_offsets<E>(sh, first, at, dx.gap, lane, offset);
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          float dz[V];
+          backward_chunk<E, RELU>(rule, in[h], gate[h], b[h], w[h], dz);
+          if (dx.p && n[h] > 0) store_chunk<E>(dx.p + offset[h], n[h], dz, HOW == Read::once);
+          sum[h] = 0.0f;
+#pragma unroll
+          for (int i = 0; i < V; ++i) sum[h] += i < n[h] ? dz[i] : 0.0f;
+        }
+      };
+      bool whole = sh.items - first - items >= 8;  // 8 elements at least lie behind
+      if (!whole) whole = readable(sh, dy, first, at, n, lane) && (!RELU || readable(sh, x, first, at, n, lane));
+      choose_read(whole, once, turn);
+      if constexpr (H == 1) {
+        if (step + lane < items) sums[wave][step + lane] = sum[0];
+      } else {  // the even lane ends with the first item's sum, the odd one with the second's
+        const bool odd = lane & 1;
+        const float total = (odd ? sum[1] : sum[0]) + lane_xor<1>(odd ? sum[0] : sum[1], lane);
+        const uint32_t it = step + (odd ? 32 : 0) + lane / 2;
+        if (it < items) sums[wave][it] = total;
+      }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const uint32_t p = lane >> mu.lane_shift, lanes = 1u << mu.lane_shift;
+    const uint32_t plane = lane >> mu.lane_shift, lanes = 1u << mu.lane_shift;
     float sum = 0.0f;
-    if (p < planes)
-      for (uint32_t i = lane & (lanes - 1); i < width; i += lanes) sum += sums[wave][p * width + i];
+    if (plane < planes)
+      for (uint32_t i = lane & (lanes - 1); i < width; i += lanes) sum += sums[wave][plane * width + i];
     for (uint32_t off = lanes / 2; off; off /= 2) sum += __shfl_xor(sum, off);
-    if (p < planes && (lane & (lanes - 1)) == 0) {
-      const uint32_t n = sh.channels.quotient(row0 + p);
-      partial[((uint64_t)segment * mu.images + n) * sh.channels.d + (row0 + p - n * sh.channels.d)] = sum;
+    if (plane < planes && (lane & (lanes - 1)) == 0) {
+      const uint32_t n = sh.channels.quotient(row0 + plane);
+      partial[((uint64_t)segment * mu.images + n) * sh.channels.d + (row0 + plane - n * sh.channels.d)] = sum;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 }
 
-// Backward of feature rows with the bias gradient: a thread keeps 8 columns and walks down rows; the threads of a
-// workgroup that share columns meet in LDS.  partial[chunk][column].
-template <Elem E>
-__global__ __launch_bounds__(kDropThreads) void dropout_features_grad_kernel(
-    DropoutShape sh, uint32_t rows, int across_shift, uint32_t rows_per_chunk, DropoutRule rule, const elem_t<E>* x, int64_t x_stride,
-    const float* __restrict__ bias, const elem_t<E>* dy, int64_t dy_stride, elem_t<E>* dx, int64_t dx_stride, float* __restrict__ partial) {
-  __shared__ float sums[kDropThreads][8];
-  const uint32_t across = 1u << across_shift, down = kDropThreads >> across_shift;
-  const uint32_t group = blockIdx.x * across + (threadIdx.x & (across - 1));
-  const uint32_t col = group * 8;
-  const bool inside = group < sh.groups32.d;
-  const int n = inside ? min(8u, sh.cols - col) : 0;
-  uint64_t seed = 0, step = 0;
-  if (rule.threshold) {
-    seed = rule.rng[0];
-    step = rule.rng[1] + rule.offset;
-  }
-  float total[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-  if (inside) {
-    float b[8];
-    load_bias(sh, bias, 0, col, n, b);
-    const uint32_t begin = blockIdx.y * rows_per_chunk, end = min(rows, begin + rows_per_chunk);
-#pragma unroll 2
-    for (uint32_t row = begin + (threadIdx.x >> across_shift); row < end; row += down) {
-      const Pack<E, 8> g = load_group<E>(dy + (int64_t)row * dy_stride + col, n);
-      Pack<E, 8> a = g;
-      if (rule.relu) a = load_group<E>(x + (int64_t)row * x_stride + col, n);
-      float dz[8];
-      backward_group<E>(rule, g, a, b, keep_bits(rule, seed, step, row, group), dz);
-      if (dx) store_group<E>(dx + (int64_t)row * dx_stride + col, n, rounded<E>(dz));
+// Backward of feature rows with the bias gradient: a lane keeps a chunk of columns and walks down rows (fp32: two at a
+// time, the pair of lanes makes the words of one each); the threads of a workgroup that share columns meet in LDS.
+// partial[chunk of rows][column].
+template <Elem E, bool RELU, Bias B>
+__global__ __launch_bounds__(kDropThreads) void dropout_features_grad_kernel(DropoutShape sh, uint32_t rows, int across_shift,
+                                                                             uint32_t rows_per_chunk, DropoutRule rule, Images<E> x,
+                                                                             const float* __restrict__ bias, Images<E> dy, Images<E> dx,
+                                                                             float* __restrict__ partial, bool once) {
+  constexpr int H = kHalves<E>, V = kChunk<E>, kRows = 2;  // rows in flight
+  __shared__ float sums[kDropThreads][V];
+  const uint32_t across = 1u << across_shift, down = kDropThreads >> across_shift, lane = threadIdx.x & 63;
+  const uint32_t col = (blockIdx.x * across + (threadIdx.x & (across - 1))) * V;
+  const int size = chunk_size<E>(sh, col);
+  float total[V] = {}, b[V];
+  if constexpr (RELU) load_bias<E, B>(sh, BiasAt(bias), 0, col, size, b);
+  const uint32_t begin = blockIdx.y * rows_per_chunk, end = min(rows, begin + rows_per_chunk);
+  for (uint32_t row0 = begin; row0 < end; row0 += kRows * down) {
+    Place at[kRows];
+    int n[kRows];
+    int64_t from[kRows], of[kRows];
+    bool behind = false;  // a chunk that reaches past a tensor's last element
 #pragma unroll
-      for (int i = 0; i < 8; ++i) total[i] += dz[i];
+    for (int r = 0; r < kRows; ++r) {
+      at[r] = {row0 + r * down + (threadIdx.x >> across_shift), col / 8, 0};
+      n[r] = at[r].row < end ? size : 0;
+      from[r] = (int64_t)at[r].row * (sh.cols + x.gap) + col;
+      of[r] = (int64_t)at[r].row * (sh.cols + dy.gap) + col;
+      behind |= n[r] > 0 && (of[r] + V > dy.span || (RELU && from[r] + V > x.span));
     }
+    const bool whole = dy.span >= V && (!RELU || x.span >= V) && __ballot(behind) == 0;
+    auto turn = [&](auto how) {
+      constexpr Read HOW = decltype(how)::value;
+      Words in[kRows], gate[kRows];
+      load_chunks<E, HOW>(dy, of, n, in);
+      if constexpr (RELU) load_chunks<E, HOW>(x, from, n, gate);
+      const Generator g(rule);
+      uint32_t w[kRows][V / 2] = {};
+      if (rule.threshold) {
+        if constexpr (H == 2) {
+          chunk_words<E>(g, at[0], at[1], lane, w);
+        } else {
+#pragma unroll
+          for (int r = 0; r < kRows; ++r) {
+            uint32_t words[1][V / 2];
+            chunk_words<E>(g, at[r], at[r], lane, words);
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) w[r][i] = words[0][i];
+          }
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        float dz[V];
+        backward_chunk<E, RELU>(rule, in[r], gate[r], b, w[r], dz);
+        if (dx.p && n[r] > 0) store_chunk<E>(dx.p + (int64_t)at[r].row * (sh.cols + dx.gap) + col, n[r], dz, HOW == Read::once);
+#pragma unroll
+        for (int i = 0; i < V; ++i) total[i] += n[r] > 0 ? dz[i] : 0.0f;
+      }
+    };
+    choose_read(whole, once, turn);
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sums[threadIdx.x][i] = total[i];
+  for (int i = 0; i < V; ++i) sums[threadIdx.x][i] = total[i];
   __syncthreads();
-  // thread t takes column t of the workgroup's, if there is one
-  for (uint32_t c = threadIdx.x; c < across * 8; c += kDropThreads) {
+  for (uint32_t c = threadIdx.x; c < across * V; c += kDropThreads) {
     float sum = 0.0f;
-    for (uint32_t d = 0; d < down; ++d) sum += sums[d * across + c / 8][c % 8];
-    const uint64_t at = (uint64_t)blockIdx.x * across * 8 + c;
+    for (uint32_t d = 0; d < down; ++d) sum += sums[d * across + c / V][c % V];
+    const uint64_t at = (uint64_t)blockIdx.x * across * V + c;
     if (at < sh.cols) partial[(uint64_t)blockIdx.y * sh.cols + at] = sum;
   }
 }

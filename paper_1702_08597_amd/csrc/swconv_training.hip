@@ -65,11 +65,22 @@ int dispatch_type(int dtype, F&& f) {
   return f(integral_constant<Elem, Elem::bf16>{});
 }
 
+template <typename F>
+int dispatch_bias(int64_t S, int64_t K, F&& f) {
+  using std::integral_constant;
+  if (S > 1) return f(integral_constant<Bias, Bias::planes>{});
+  return K % 8 == 0 ? f(integral_constant<Bias, Bias::columns>{}) : f(integral_constant<Bias, Bias::ragged>{});
+}
+
 // Rows of `span` elements, `stride` apart.
 struct Rows {
   const void* p;
   int64_t rows, span, stride;
 };
+template <Elem E>
+Images<E> images(const Rows& a) {
+  return {(elem_t<E>*)a.p, a.stride - a.span, (a.rows - 1) * a.stride + a.span};
+}
 bool placed(const Rows& a, int64_t size) { return a.p && (uintptr_t)a.p % size == 0; }
 // An output may be the input itself, or share no element with it (one row may lie between two of the other's).
 bool may_write(const Rows& out, const Rows& in, int64_t size) {
@@ -104,9 +115,17 @@ int image_stride(int64_t N, int64_t K, int64_t S, int64_t given, int64_t* stride
   return *stride > kMost || (N > 1 && (N - 1) > kMost / *stride) ? SWCONV_EUNSUPPORTED : SWCONV_OK;
 }
 
-DropoutShape shape_of(int64_t N, int64_t K, int64_t S) {
-  const int64_t rows = S == 1 ? N : N * K, cols = S == 1 ? K : S, groups = (cols + 7) / 8;
-  return {Divisor((uint64_t)groups), Divisor32((uint32_t)groups), Divisor32((uint32_t)K), (uint64_t)(rows * groups), (uint32_t)cols, S == 1};
+DropoutShape shape_of(int dtype, int64_t N, int64_t K, int64_t S) {
+  const int64_t rows = S == 1 ? N : N * K, cols = S == 1 ? K : S, groups = (cols + 7) / 8, channels = S == 1 ? 1 : K;
+  const uint32_t items = dtype == SWCONV_F32 ? 32 : 64;
+  return {Divisor((uint64_t)groups), Divisor32((uint32_t)groups), Divisor32((uint32_t)channels), (uint64_t)(rows * groups), (uint32_t)cols,
+          (uint32_t)(8 * groups - cols), (uint32_t)(items % groups), (uint32_t)(items / groups)};
+}
+
+template <Elem E>
+dim3 item_grid(const DropoutShape& sh) {
+  const int64_t turn = kDropThreads * kDropSteps<E>;
+  return dim3((unsigned)std::min<int64_t>(((int64_t)sh.items + turn - 1) / turn, kMaxGroups));
 }
 
 int rule_of(int64_t N, int relu, float p, const uint64_t* rng, uint64_t offset, DropoutRule* rule) {
@@ -117,12 +136,11 @@ int rule_of(int64_t N, int relu, float p, const uint64_t* rng, uint64_t offset, 
   return SWCONV_OK;
 }
 
-// How the bias gradient is summed: partial sums in `parts` rows of K.
+// How the bias gradient is summed: partial sums in `parts` rows of K (whatever the type).
 struct BiasParts {
   int64_t parts;
   MapUnits units{0, Divisor32(1), 0, 0, 1, 6};
-  int across_shift = 0;
-  int64_t col_blocks = 1, rows_per_chunk = 1;
+  int64_t rows_per_chunk = 1;
 };
 BiasParts bias_parts(int64_t N, int64_t K, int64_t S) {
   BiasParts b;
@@ -134,13 +152,12 @@ BiasParts bias_parts(int64_t N, int64_t K, int64_t S) {
                6 - ceil_log2(planes)};
     b.parts = N * segments;
   } else {
-    b.across_shift = std::min(8, ceil_log2(groups));
-    const int64_t across = (int64_t)1 << b.across_shift, down = kDropThreads / across;
-    b.col_blocks = (groups + across - 1) / across;
-    // 1024 workgroups, of at least 4 rows a thread
-    const int64_t chunks = std::clamp<int64_t>((N + 4 * down - 1) / (4 * down), 1, std::max<int64_t>(1, 1024 / b.col_blocks));
-    b.rows_per_chunk = (N + chunks - 1) / std::max<int64_t>(chunks, 1);
-    b.parts = b.rows_per_chunk ? (N + b.rows_per_chunk - 1) / b.rows_per_chunk : 0;
+    // 1024 workgroups of the 16-bit types, of at least 4 rows a thread
+    const int64_t across = std::min<int64_t>(kDropThreads, (int64_t)1 << ceil_log2(groups)), down = kDropThreads / across;
+    const int64_t col_blocks = (groups + across - 1) / across;
+    const int64_t chunks = std::clamp<int64_t>((N + 4 * down - 1) / (4 * down), 1, std::max<int64_t>(1, 1024 / col_blocks));
+    b.rows_per_chunk = std::max<int64_t>(1, (N + chunks - 1) / chunks);
+    b.parts = (N + b.rows_per_chunk - 1) / b.rows_per_chunk;
   }
   return b;
 }
@@ -169,7 +186,7 @@ struct Parts {
 };
 Parts parts_of(int dtype, int64_t rows, int64_t classes, int top) {
   const int64_t tile = 64 * (16 / size_of(dtype)) * kLogpUnroll, tiles = (classes + tile - 1) / tile;
-  if (tiles <= 2 || (rows >= 1024 && tiles * 96 <= rows && (tiles <= 8 || top <= 8))) return {1, 1, classes};
+  if (tiles <= 2 || (rows >= 1024 && tiles * (top ? 64 : 96) <= rows && (tiles <= 8 || top <= 8))) return {1, 1, classes};
   if (rows > 256 || tiles < 12) return {4, 1, classes};
   int64_t parts = 1;
   if (rows > 0 && rows <= 128)
@@ -200,13 +217,15 @@ int swconv_dropout_forward(int dtype, int64_t N, int64_t K, int64_t S, const voi
   if (!placed(x, size) || !placed(y, size) || !may_write(y, x, size) || (uintptr_t)bias_dev % 4) return SWCONV_EINVAL;
   const hipStream_t st = (hipStream_t)hip_stream;
   const StreamDevice device(st);
-  const DropoutShape sh = shape_of(N, K, S);
-  const int64_t turn = kDropThreads * kDropItems;
-  const dim3 grid((unsigned)std::min<int64_t>(((int64_t)sh.items + turn - 1) / turn, kMaxGroups));
+  const DropoutShape sh = shape_of(dtype, N, K, S);
+  const bool once = 2 * N * K * S * size > kCacheBytes;
   return dispatch_type(dtype, [&](auto e) {
     constexpr Elem E = decltype(e)::value;
-    return launch(dropout_kernel<E, false>, grid, kDropThreads, st, sh, rule, (const elem_t<E>*)x_dev, x_stride, bias_dev,
-                  (const elem_t<E>*)nullptr, (int64_t)0, (elem_t<E>*)y_dev, y_stride);
+    const dim3 grid = item_grid<E>(sh);
+    return dispatch_bias(S, K, [&](auto by) {
+      return launch(dropout_kernel<E, Pass::forward, decltype(by)::value>, grid, kDropThreads, st, sh, rule, images<E>(x), bias_dev,
+                    Images<E>{}, images<E>(y), once);
+    });
   });
 }
 
@@ -242,27 +261,36 @@ int swconv_dropout_backward(int dtype, int64_t N, int64_t K, int64_t S, const vo
   const Rows dy{dy_dev, N, K * S, dy_stride}, x{relu ? x_dev : nullptr, N, K * S, x_stride}, dx{dx_dev, N, K * S, dx_stride};
   if (!placed(dy, size) || (relu && !placed(x, size)) || (!dx_dev && !dbias_dev)) return SWCONV_EINVAL;
   if (dx_dev && (!placed(dx, size) || !may_write(dx, dy, size) || !may_write(dx, x, size))) return SWCONV_EINVAL;
-  const DropoutShape sh = shape_of(N, K, S);
+  const DropoutShape sh = shape_of(dtype, N, K, S);
   if (dbias_dev && bp.parts > 1 && (!workspace_dev || workspace_bytes < bp.parts * K * (int64_t)sizeof(float))) return SWCONV_EINVAL;
   float* partial = bp.parts > 1 ? (float*)workspace_dev : dbias_dev;
+  const bool once = (relu ? 3 : 2) * N * K * S * size > kCacheBytes;
   const StreamDevice device(st);
   rc = dispatch_type(dtype, [&](auto e) {
     constexpr Elem E = decltype(e)::value;
-    const auto *g = (const elem_t<E>*)dy_dev, *a = (const elem_t<E>*)x_dev;
-    auto* d = (elem_t<E>*)dx_dev;
+    const Images<E> g = images<E>(dy), a = images<E>(x), d = images<E>(dx);
     if (!dbias_dev) {
-      const int64_t turn = kDropThreads * kDropItems;
-      const dim3 grid((unsigned)std::min<int64_t>(((int64_t)sh.items + turn - 1) / turn, kMaxGroups));
-      return launch(dropout_kernel<E, true>, grid, kDropThreads, st, sh, rule, a, x_stride, bias_dev, g, dy_stride, d, dx_stride);
+      const dim3 grid = item_grid<E>(sh);
+      if (!relu)
+        return launch(dropout_kernel<E, Pass::backward, Bias::planes>, grid, kDropThreads, st, sh, rule, a, bias_dev, g, d, once);
+      return dispatch_bias(S, K, [&](auto by) {
+        return launch(dropout_kernel<E, Pass::backward_relu, decltype(by)::value>, grid, kDropThreads, st, sh, rule, a, bias_dev, g, d, once);
+      });
     }
     if (S > 1) {
       const int64_t waves = kDropThreads / 64;
       const dim3 grid((unsigned)std::min<int64_t>(((int64_t)bp.units.units + waves - 1) / waves, kMaxGroups));
-      return launch(dropout_maps_grad_kernel<E>, grid, kDropThreads, st, sh, bp.units, rule, a, x_stride, bias_dev, g, dy_stride, d,
-                    dx_stride, partial);
+      return launch(relu ? dropout_maps_grad_kernel<E, true> : dropout_maps_grad_kernel<E, false>, grid, kDropThreads, st, sh, bp.units, rule, a,
+                    bias_dev, g, d, partial, once);
     }
-    return launch(dropout_features_grad_kernel<E>, dim3((unsigned)bp.col_blocks, (unsigned)bp.parts), kDropThreads, st, sh, (uint32_t)N,
-                  bp.across_shift, (uint32_t)bp.rows_per_chunk, rule, a, x_stride, bias_dev, g, dy_stride, d, dx_stride, partial);
+    const int64_t chunks = (K + 7) / 8 * kHalves<E>;  // of 16 bytes
+    const int across_shift = std::min(8, ceil_log2(chunks));
+    const dim3 grid((unsigned)((chunks + (1 << across_shift) - 1) >> across_shift), (unsigned)bp.parts);
+    auto kernel = !relu        ? dropout_features_grad_kernel<E, false, Bias::columns>
+                  : K % 8 == 0 ? dropout_features_grad_kernel<E, true, Bias::columns>
+                               : dropout_features_grad_kernel<E, true, Bias::ragged>;
+    return launch(kernel, grid, kDropThreads, st, sh, (uint32_t)N, across_shift, (uint32_t)bp.rows_per_chunk, rule, a, bias_dev, g, d, partial,
+                  once);
   });
   if (rc || !dbias_dev || bp.parts == 1) return rc;
   return launch(bias_grad_kernel, sum_grid, kBiasCols * kBiasDown, st, (const float*)partial, (uint32_t)bp.parts, (uint32_t)K, dbias_dev);
