@@ -243,29 +243,54 @@ __device__ __forceinline__ void backward_chunk(const DropoutRule& rule, const Wo
 // Forward, and backward without a bias gradient: waves over all items in the order of memory.  Bound by memory: a chunk in
 // (two with ReLU backward) and a chunk out.  GATE: the backward pass reads x for the ReLU.
 enum class Pass { forward, backward, backward_relu };
-template <Elem E, Pass PASS, Bias B, Read HOW>
+template <Elem E>
+constexpr int kTurnChunks = kDropSteps<E> * kHalves<E>;
+
+// The chunks of a wave's turn: their items, and how many columns of each there are.
+template <Elem E>
+__device__ __forceinline__ void turn_places(const DropoutShape& sh, uint64_t first, int lane, Place (&at)[kTurnChunks<E>]) {
+  at[0] = place_at(sh, first, lane_item<E>(lane));
+#pragma unroll
+  for (int c = 1; c < kTurnChunks<E>; ++c) at[c] = next_place<64 / kHalves<E>>(sh, at[c - 1]);
+}
+
+// DENSE: rows of whole items and no gaps anywhere.  Then a chunk lies where its number says, and the loads go out before the
+// places are worked out (which takes as long, with eight waves to a SIMD, as the loads).
+template <Elem E, Pass PASS, Bias B, Read HOW, bool DENSE>
 __device__ __forceinline__ void dropout_turn(const DropoutShape& sh, const DropoutRule& rule, const Images<E>& x, const float* bias,
-                                             const Images<E>& dy, const Images<E>& out, uint64_t first,
-                                             const Place (&at)[kDropSteps<E> * kHalves<E>], const int (&n)[kDropSteps<E> * kHalves<E>],
-                                             int lane) {
-  constexpr int H = kHalves<E>, V = kChunk<E>, COUNT = kDropSteps<E> * H;
+                                             const Images<E>& dy, const Images<E>& out, uint64_t first, uint32_t left,
+                                             Place (&at)[kTurnChunks<E>], int lane) {
+  constexpr int H = kHalves<E>, V = kChunk<E>, COUNT = kTurnChunks<E>;
   Words in[COUNT], gate[COUNT];
   int64_t offset[COUNT];
+  int n[COUNT];
   float b[COUNT][V];
   const Images<E>& from = PASS == Pass::forward ? x : dy;
-  chunk_offsets<E>(sh, first, at, from.gap, lane, offset);
+  if constexpr (DENSE) {
+#pragma unroll
+    for (int c = 0; c < COUNT; ++c) {
+      const uint32_t ahead = lane_item<E>(lane) + c * (64 / H);
+      offset[c] = (int64_t)(first * 8) + (ahead * 8 + (H == 1 ? 0 : (lane & 1) * 4));
+      n[c] = ahead < left ? V : 0;
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < COUNT; ++c) n[c] = at[c].ahead < left ? chunk_size<E>(sh, first_column<E>(at[c], lane)) : 0;
+    chunk_offsets<E>(sh, first, at, from.gap, lane, offset);
+  }
   load_chunks<E, HOW>(from, offset, n, in);
   if constexpr (PASS == Pass::backward_relu) {
-    if (x.gap != dy.gap) chunk_offsets<E>(sh, first, at, x.gap, lane, offset);
+    if (!DENSE && x.gap != dy.gap) chunk_offsets<E>(sh, first, at, x.gap, lane, offset);
     load_chunks<E, HOW>(x, offset, n, gate);
   }
+  if constexpr (DENSE) turn_places<E>(sh, first, lane, at);
   if constexpr (PASS != Pass::backward) {
     const BiasAt by(bias);
 #pragma unroll
     for (int c = 0; c < COUNT; ++c) load_bias<E, B>(sh, by, at[c].row, first_column<E>(at[c], lane), n[c], b[c]);
   }
   const Generator g(rule);
-  if (out.gap != (PASS == Pass::backward_relu ? x.gap : from.gap)) chunk_offsets<E>(sh, first, at, out.gap, lane, offset);
+  if (!DENSE && out.gap != (PASS == Pass::backward_relu ? x.gap : from.gap)) chunk_offsets<E>(sh, first, at, out.gap, lane, offset);
 #pragma unroll
   for (int s = 0; s < kDropSteps<E>; ++s) {
     uint32_t w[H][V / 2] = {};
@@ -284,26 +309,30 @@ __device__ __forceinline__ void dropout_turn(const DropoutShape& sh, const Dropo
 }
 template <Elem E, Pass PASS, Bias B>
 __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutShape sh, DropoutRule rule, Images<E> x, const float* __restrict__ bias,
-                                                               Images<E> dy, Images<E> out, bool once) {
-  constexpr int H = kHalves<E>, COUNT = kDropSteps<E> * H;
+                                                               Images<E> dy, Images<E> out, bool dense, bool once) {
+  constexpr int COUNT = kTurnChunks<E>;
   const int lane = threadIdx.x & 63;
   const uint64_t wave = (uint64_t)blockIdx.x * (kDropThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   for (uint64_t first = wave * (64 * kDropSteps<E>); first < sh.items; first += (uint64_t)gridDim.x * (kDropThreads * kDropSteps<E>)) {
     const uint32_t left = (uint32_t)min(sh.items - first, (uint64_t)(64 * kDropSteps<E>));
     Place at[COUNT];
-    int n[COUNT];
-    Place p = place_at(sh, first, lane_item<E>(lane));
-#pragma unroll
-    for (int c = 0; c < COUNT; ++c) {
-      if (c) p = next_place<64 / H>(sh, p);
-      at[c] = p;
-      n[c] = p.ahead < left ? chunk_size<E>(sh, first_column<E>(p, lane)) : 0;
+    if (dense) {
+      if (once)
+        dropout_turn<E, PASS, B, Read::once, true>(sh, rule, x, bias, dy, out, first, left, at, lane);
+      else
+        dropout_turn<E, PASS, B, Read::whole, true>(sh, rule, x, bias, dy, out, first, left, at, lane);
+      continue;
     }
+    turn_places<E>(sh, first, lane, at);
     bool whole = sh.items - first - left >= 8;  // 8 elements at least lie behind
-    if (!whole)
+    if (!whole) {
+      int n[COUNT];
+#pragma unroll
+      for (int c = 0; c < COUNT; ++c) n[c] = at[c].ahead < left ? 1 : 0;
       whole = (PASS == Pass::backward || readable(sh, x, first, at, n, lane)) && (PASS == Pass::forward || readable(sh, dy, first, at, n, lane));
+    }
     choose_read(whole, once, [&](auto how) {
-      dropout_turn<E, PASS, B, decltype(how)::value>(sh, rule, x, bias, dy, out, first, at, n, lane);
+      dropout_turn<E, PASS, B, decltype(how)::value, false>(sh, rule, x, bias, dy, out, first, left, at, lane);
     });
   }
 }

@@ -219,12 +219,13 @@ int swconv_dropout_forward(int dtype, int64_t N, int64_t K, int64_t S, const voi
   const StreamDevice device(st);
   const DropoutShape sh = shape_of(dtype, N, K, S);
   const bool once = 2 * N * K * S * size > kCacheBytes;
+  const bool dense = sh.pad == 0 && x_stride == K * S && y_stride == K * S;
   return dispatch_type(dtype, [&](auto e) {
     constexpr Elem E = decltype(e)::value;
     const dim3 grid = item_grid<E>(sh);
     return dispatch_bias(S, K, [&](auto by) {
       return launch(dropout_kernel<E, Pass::forward, decltype(by)::value>, grid, kDropThreads, st, sh, rule, images<E>(x), bias_dev,
-                    Images<E>{}, images<E>(y), once);
+                    Images<E>{}, images<E>(y), dense, once);
     });
   });
 }
@@ -265,6 +266,7 @@ int swconv_dropout_backward(int dtype, int64_t N, int64_t K, int64_t S, const vo
   if (dbias_dev && bp.parts > 1 && (!workspace_dev || workspace_bytes < bp.parts * K * (int64_t)sizeof(float))) return SWCONV_EINVAL;
   float* partial = bp.parts > 1 ? (float*)workspace_dev : dbias_dev;
   const bool once = (relu ? 3 : 2) * N * K * S * size > kCacheBytes;
+  const bool dense = sh.pad == 0 && dy_stride == K * S && dx_stride == K * S && (!relu || x_stride == K * S);
   const StreamDevice device(st);
   rc = dispatch_type(dtype, [&](auto e) {
     constexpr Elem E = decltype(e)::value;
@@ -272,9 +274,9 @@ int swconv_dropout_backward(int dtype, int64_t N, int64_t K, int64_t S, const vo
     if (!dbias_dev) {
       const dim3 grid = item_grid<E>(sh);
       if (!relu)
-        return launch(dropout_kernel<E, Pass::backward, Bias::planes>, grid, kDropThreads, st, sh, rule, a, bias_dev, g, d, once);
+        return launch(dropout_kernel<E, Pass::backward, Bias::planes>, grid, kDropThreads, st, sh, rule, a, bias_dev, g, d, dense, once);
       return dispatch_bias(S, K, [&](auto by) {
-        return launch(dropout_kernel<E, Pass::backward_relu, decltype(by)::value>, grid, kDropThreads, st, sh, rule, a, bias_dev, g, d, once);
+        return launch(dropout_kernel<E, Pass::backward_relu, decltype(by)::value>, grid, kDropThreads, st, sh, rule, a, bias_dev, g, d, dense, once);
       });
     }
     if (S > 1) {
