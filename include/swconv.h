@@ -366,7 +366,7 @@ typedef enum {
  *   offset      added to the step count (mod 2^64), e.g. the number of the layer.  Calls of equal seed and step + offset
  *               and equal shape make equal masks.
  *   y_dev       DEVICE, N x K x S with y_stride; may be x_dev with the same stride, else shares no element with x.
- *               Elements between the images are neither read nor written.
+ *               What lies between the images is not written, and what it holds does not matter.
  * The mask is a function of the sizes and the four numbers alone, whatever dtype, strides and launch: with
  * row = n*K + k, col = s (S = 1: row = n, col = k) an element is kept if the 16-bit field col % 8 (low half of word 0
  * first) of philox4x32-10 at counter {col / 8, row, low and high word of step + offset} with the seed as key is not

@@ -9,7 +9,9 @@ namespace swconv {
 // The value of lane ^ OFF by moves within the vector unit: a trip through LDS takes ten times as long.
 template <int OFF>
 __device__ __forceinline__ uint32_t lane_xor(uint32_t v, int lane) {
-  auto dpp = [](uint32_t a, auto control) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, decltype(control)::value, 0xf, 0xf, true); };
+  auto dpp = [](uint32_t a, auto control) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, decltype(control)::value, 0xf, 0xf, true);
+  };
   using std::integral_constant;
   if constexpr (OFF == 1) return dpp(v, integral_constant<int, 0xB1>{});         // quad_perm 1 0 3 2
   else if constexpr (OFF == 2) return dpp(v, integral_constant<int, 0x4E>{});    // quad_perm 2 3 0 1

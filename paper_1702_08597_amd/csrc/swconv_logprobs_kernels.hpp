@@ -1,15 +1,19 @@
 // HIP kernels of the log probabilities at a network's end.  For a row of scores x_j:
 //   m = max x_j,  s = sum exp(x_j - m),  ls = log s,  log p_j = (x_j - m) - ls,  H = -sum p_j log p_j
-// and H = ls - (sum (x_j - m) exp(x_j - m)) / s, whose two terms are both positive.  One pass over the scores: every lane
-// keeps the largest score it has seen and both sums relative to it, scaled when that one changes; lanes, waves and
-// parts of a row are joined in the same way.  All of it in fp32 whatever the scores' type.
+// and H = ls - (sum (x_j - m) exp(x_j - m)) / s, whose two terms are both positive.  One pass over the scores: every wave
+// keeps the largest score it has seen, its lanes both sums relative to it, scaled when that one changes; waves and parts of a
+// row are joined in the same way.  All of it in fp32 whatever the scores' type.
 //   d x_j = g ([j = label] - p_j) - h p_j (log p_j + H)
 // A class of score -inf is masked: exp gives 0, and it never is among the best.  NaN and +inf make the row's largest
 // score NaN or +inf (the maximum used propagates NaN), from which the row's results are made NaN.
 // The best t classes, t <= 64: the pass over the scores only notes the largest one of each lane and segment (16 to a wave's
 // share of a row).  The t-th largest of the lanes' largest scores is a bar that t scores reach and few others: the lanes and
 // segments that reach it are read again, a lane to a score, and what reaches it is sorted, as 64-bit keys (score, then
-// the lower class), one to a lane.
+// the lower class), one to a lane.  (Keeping the best up to date within the pass, 4096 x 131072 bf16 took 239 us for the best
+// one and 413 for 64; so it takes 207 and 242, without any 182.)
+// What bounds the forward pass: memory for many long rows - 4096 x 131072 bf16 with entropies at 5.9 TB/s, five vector
+// instructions and an exponential to a score, which is 80 % of what the vector units issue; the way through one wave's
+// tile, sorts and joins for few rows (1 x 32768 10 us, 256 x 1000 with the best 5 7 us, 4.5 without any).
 #pragma once
 #include "swconv_elements.hpp"
 #include "swconv_lanes.hpp"
@@ -21,8 +25,6 @@ constexpr int kTopMax = 64;           // one lane each
 constexpr float kFarBelow = -256.0f;  // exp(-256) is 0 in fp32; keeps 0 * inf out of the sums
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 constexpr float kLowest = -3.402823466e38f;
-
-__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 // ---- lanes ------------------------------------------------------------------------------------------------------
 // The calling lane's number among those of a mask.
@@ -80,8 +82,8 @@ struct RowSums {
 };
 
 // exp(x - m) for x < m as 2^(x log2 e - c) with c = m log2 e rounded: one fused multiply-add whose only error is its own
-// rounding; what c is off by (less than 64) is put right once per row (finish_row).  From 2^30 on the next lower score is 128
-// further down, where exp gives 0: so does c = inf.
+// rounding; what c is off by (at most 64) is put right once per row (finish_row).  From 2^30 on the next lower score is at least
+// 64 further down, where exp is nothing next to 1: c = inf makes it 0.
 __device__ __forceinline__ float reference(float m) { return fabsf(m) >= 1073741824.0f ? INFINITY : m * kLog2e; }
 
 // The sums relative to a larger score m, which makes the scores that were largest ordinary ones.
@@ -159,8 +161,9 @@ struct TopList {
 // reaches bar(): a lane's scores of a tile are U runs of V.  `owners`: LDS, room for 128 (segment, lane) pairs; all of
 // them are read in one go, 64 scores at a time and four such reads in flight.
 template <Elem E, typename Bar, typename See>
-__device__ __forceinline__ void look_again(const elem_t<E>* x_row, const float (*segment_max)[64], uint16_t* owners, int segments,
-                                           int segment_tiles, int64_t first, int64_t step, int64_t end, int lane, Bar&& bar, See&& see) {
+__device__ __forceinline__ void look_again(const elem_t<E>* x_row, const float (*segment_max)[64], uint16_t* owners,
+                                           int segments, int segment_tiles, int64_t first, int64_t step, int64_t end,
+                                           int lane, Bar&& bar, See&& see) {
   constexpr int V = kWordsElems<E>, U = kLogpUnroll, kFlight = 4;
   int n = 0;
   for (int s = 0; s < segments; ++s) {
@@ -209,8 +212,8 @@ __device__ __forceinline__ Label label_at(int32_t at, const elem_t<E>* x_row, in
 
 // A row's results from its sums and its best classes; called by one wave.
 template <Elem E>
-__device__ __forceinline__ void finish_row(const LogprobsOut& out,
-                                           int64_t row, Label label, const RowSums& a, TopKey best, int top, int lane) {
+__device__ __forceinline__ void finish_row(const LogprobsOut& out, int64_t row, Label label, const RowSums& a,
+                                           TopKey best, int top, int lane) {
   const bool poisoned = !(a.m <= -kLowest);  // NaN or +inf among the scores
   const bool empty = a.n == 0.0f && !poisoned;
   // m log2 e = c + off: every exponential, 2^(x log2 e - c), is 2^off too large, its logarithm off too high
@@ -271,7 +274,8 @@ __device__ __forceinline__ int64_t group_start(int64_t tile, int u, int64_t end,
   return min(tile + (u * 64 + lane) * kWordsElems<E>, max(end - kWordsElems<E>, (int64_t)0));
 }
 template <Elem E>
-__device__ __forceinline__ void load_tile(Words (&raw)[kLogpUnroll], const elem_t<E>* x_row, int64_t tile, int64_t end, int lane, bool once) {
+__device__ __forceinline__ void load_tile(Words (&raw)[kLogpUnroll], const elem_t<E>* x_row, int64_t tile, int64_t end,
+                                          int lane, bool once) {
   constexpr int V = kWordsElems<E>, U = kLogpUnroll;
   if (tile + 64 * V * U <= end) {
     const elem_t<E>* p = x_row + tile + lane * V;
@@ -298,10 +302,10 @@ __device__ __forceinline__ void load_tile(Words (&raw)[kLogpUnroll], const elem_
 // wave keep their sums relative to one score, the largest that the wave has seen: it changes in every i-th tile or so,
 // and the other tiles take no scaling.
 template <Elem E, int WAVES, bool TOP, bool ENTROPY>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void logprobs_kernel(int64_t rows, int64_t classes, const elem_t<E>* __restrict__ scores,
-                                                                int64_t row_stride, const int32_t* __restrict__ labels, int top,
-                                                                int parts, int64_t part_classes, bool once, LogprobsOut out,
-                                                                RowSums* __restrict__ part_sums, TopKey* __restrict__ part_keys) {
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void logprobs_kernel(
+    int64_t rows, int64_t classes, const elem_t<E>* __restrict__ scores, int64_t row_stride,
+    const int32_t* __restrict__ labels, int top, int parts, int64_t part_classes, bool once, LogprobsOut out,
+    RowSums* __restrict__ part_sums, TopKey* __restrict__ part_keys) {
   constexpr int V = kWordsElems<E>, U = kLogpUnroll, kWaves = WAVES == 1 ? 4 : WAVES, kTile = 64 * V * U;
   __shared__ TopKey lists[TOP ? kWaves : 1][kWaiting];
   __shared__ float segment_max[TOP ? kWaves : 1][kSegments][64];
@@ -338,12 +342,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void logprobs_kernel
       if (__ballot(!(lane_max < a.m)) == 0) {
 #pragma unroll
         for (int k = 0; k < U * V; ++k) {
-          const float d = fmaxf(__builtin_fmaf(word_elem<E>(raw[k / V], k % V), kLog2e, -c), kFarBelow), e = __builtin_amdgcn_exp2f(d);
+          const float x = word_elem<E>(raw[k / V], k % V);
+          const float d = fmaxf(__builtin_fmaf(x, kLog2e, -c), kFarBelow), e = __builtin_amdgcn_exp2f(d);
           a.s += e;
           if constexpr (ENTROPY) a.t += d * e;
         }
       } else {
-        const float m = reduce_lanes(__builtin_elementwise_maximum(lane_max, a.m), lane, [](float x, float y) { return __builtin_elementwise_maximum(x, y); });
+        auto larger = [](float x, float y) { return __builtin_elementwise_maximum(x, y); };
+        const float m = reduce_lanes(larger(lane_max, a.m), lane, larger);
         if (!(m == a.m)) {
           a.n = lane == 0 ? n : 0.0f;
           a = raised(a, m);
@@ -421,7 +427,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void logprobs_kernel
         if (n <= kWaiting) {
           if (wave == 0) {
             list.best = sort_lanes(lane < n ? all[lane] : (TopKey)0, lane, n);
-            if (n > 64) list.best = merge_lanes(list.best, sort_lanes(lane < n - 64 ? all[64 + lane] : (TopKey)0, lane, n - 64), lane);
+            if (n > 64) {
+              const TopKey rest = sort_lanes(lane < n - 64 ? all[64 + lane] : (TopKey)0, lane, n - 64);
+              list.best = merge_lanes(list.best, rest, lane);
+            }
           }
         } else {
           __syncthreads();  // all have read `waiting`
@@ -473,7 +482,8 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(int64_t rows, int64_
 
 // ---- backward ---------------------------------------------------------------------------------------------------
 // With e = exp(x - m) and p = e exp(-ls):  d x = -p (g + h (x - m - ls + H)) = e (b + a log2 e), a and b by row.  The
-// exponent holds x - m alone: ls in it would cost the digits of its size.
+// exponent holds x - m alone: ls in it would cost the digits of its size.  Bound by memory: 4096 x 131072 bf16 at 6.1 TB/s
+// read and written.
 struct GradRow {
   float m, a, b, g;
   int32_t label;
@@ -491,7 +501,8 @@ __device__ __forceinline__ GradRow grad_row(const GradIn& in, int64_t row, int64
   const float g = in.dlogprob ? in.dlogprob[row] : 0.0f;
   r.g = !in.dlogprob || r.label < 0 ? 0.0f : r.label < classes ? g : NAN;
   const float h = in.dentropy ? in.dentropy[row] : 0.0f, H = in.dentropy ? in.entropy[row] : 0.0f;
-  const float scale = -__builtin_amdgcn_exp2f(-ls * kLog2e);
+  const float u = ls * kLog2e, low = __builtin_fmaf(ls, kLog2e, -u);  // exp(-ls) to the digits of ls, not of u
+  const float scale = -__builtin_amdgcn_exp2f(-u) * __builtin_fmaf(-low, kLn2, 1.0f);
   r.a = scale * h * kLn2;
   r.b = scale * (r.g + h * (H - ls));
   r.plain = fabsf(r.m) < INFINITY && fabsf(r.a) < INFINITY && fabsf(r.b) < INFINITY;
@@ -549,8 +560,10 @@ constexpr int kGradThreads = 256;
 template <Elem E>
 constexpr int kGradUnroll = E == Elem::f32 ? 1 : 2;
 template <Elem E, bool ENTROPY>
-__global__ __launch_bounds__(kGradThreads) void logprobs_grad_kernel(int64_t rows, int64_t classes, const elem_t<E>* scores, int64_t row_stride,
-                                                                     GradIn in, bool once, elem_t<E>* out, int64_t out_stride) {
+__global__ __launch_bounds__(kGradThreads) void logprobs_grad_kernel(int64_t rows, int64_t classes,
+                                                                     const elem_t<E>* scores, int64_t row_stride,
+                                                                     GradIn in, bool once, elem_t<E>* out,
+                                                                     int64_t out_stride) {
   constexpr int V = kWordsElems<E>, U = kGradUnroll<E>;
   const int64_t j = ((int64_t)blockIdx.x * (kGradThreads * U) + threadIdx.x) * V;
   for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {

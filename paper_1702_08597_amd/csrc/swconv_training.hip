@@ -118,8 +118,9 @@ int image_stride(int64_t N, int64_t K, int64_t S, int64_t given, int64_t* stride
 DropoutShape shape_of(int dtype, int64_t N, int64_t K, int64_t S) {
   const int64_t rows = S == 1 ? N : N * K, cols = S == 1 ? K : S, groups = (cols + 7) / 8, channels = S == 1 ? 1 : K;
   const uint32_t items = dtype == SWCONV_F32 ? 32 : 64;
-  return {Divisor((uint64_t)groups), Divisor32((uint32_t)groups), Divisor32((uint32_t)channels), (uint64_t)(rows * groups), (uint32_t)cols,
-          (uint32_t)(8 * groups - cols), (uint32_t)(items % groups), (uint32_t)(items / groups)};
+  return {Divisor((uint64_t)groups),       Divisor32((uint32_t)groups),   Divisor32((uint32_t)channels),
+          (uint64_t)(rows * groups),       (uint32_t)cols,                (uint32_t)(8 * groups - cols),
+          (uint32_t)(items % groups),      (uint32_t)(items / groups)};
 }
 
 template <Elem E>
@@ -148,8 +149,8 @@ BiasParts bias_parts(int64_t N, int64_t K, int64_t S) {
   if (S > 1) {
     const int64_t segments = (groups + kDropUnit - 1) / kDropUnit;
     const int planes = (int)std::clamp<int64_t>(kDropUnit / groups, 1, 64);
-    b.units = {(uint64_t)((N * K + planes - 1) / planes * segments), Divisor32((uint32_t)segments), (uint32_t)(N * K), (uint32_t)N, planes,
-               6 - ceil_log2(planes)};
+    b.units = {(uint64_t)((N * K + planes - 1) / planes * segments), Divisor32((uint32_t)segments), (uint32_t)(N * K),
+               (uint32_t)N, planes, 6 - ceil_log2(planes)};
     b.parts = N * segments;
   } else {
     // 1024 workgroups of the 16-bit types, of at least 4 rows a thread
@@ -203,8 +204,9 @@ int64_t parts_bytes(const Parts& p, int64_t rows, int top) {
 
 extern "C" {
 
-int swconv_dropout_forward(int dtype, int64_t N, int64_t K, int64_t S, const void* x_dev, int64_t x_stride, const float* bias_dev, int relu,
-                           float p, const uint64_t* rng_dev, uint64_t offset, void* hip_stream, void* y_dev, int64_t y_stride) {
+int swconv_dropout_forward(int dtype, int64_t N, int64_t K, int64_t S, const void* x_dev, int64_t x_stride,
+                           const float* bias_dev, int relu, float p, const uint64_t* rng_dev, uint64_t offset,
+                           void* hip_stream, void* y_dev, int64_t y_stride) {
   int rc;
   DropoutRule rule;
   if (!known_type(dtype)) return SWCONV_EINVAL;
@@ -224,8 +226,8 @@ int swconv_dropout_forward(int dtype, int64_t N, int64_t K, int64_t S, const voi
     constexpr Elem E = decltype(e)::value;
     const dim3 grid = item_grid<E>(sh);
     return dispatch_bias(S, K, [&](auto by) {
-      return launch(dropout_kernel<E, Pass::forward, decltype(by)::value>, grid, kDropThreads, st, sh, rule, images<E>(x), bias_dev,
-                    Images<E>{}, images<E>(y), dense, once);
+      return launch(dropout_kernel<E, Pass::forward, decltype(by)::value>, grid, kDropThreads, st, sh, rule,
+                    images<E>(x), bias_dev, Images<E>{}, images<E>(y), dense, once);
     });
   });
 }
@@ -252,7 +254,7 @@ int swconv_dropout_backward(int dtype, int64_t N, int64_t K, int64_t S, const vo
   if ((uintptr_t)bias_dev % 4 || (uintptr_t)dbias_dev % 4 || (uintptr_t)workspace_dev % 4) return SWCONV_EINVAL;
   const hipStream_t st = (hipStream_t)hip_stream;
   const BiasParts bp = bias_parts(N, K, S);
-  const dim3 sum_grid((unsigned)((K + kBiasCols - 1) / kBiasCols));
+  const dim3 sum_grid((unsigned)std::min<int64_t>((K + kBiasCols - 1) / kBiasCols, kMaxGroups));
   if (N == 0) {
     if (!dbias_dev) return SWCONV_OK;
     const StreamDevice device(st);
@@ -263,7 +265,9 @@ int swconv_dropout_backward(int dtype, int64_t N, int64_t K, int64_t S, const vo
   if (!placed(dy, size) || (relu && !placed(x, size)) || (!dx_dev && !dbias_dev)) return SWCONV_EINVAL;
   if (dx_dev && (!placed(dx, size) || !may_write(dx, dy, size) || !may_write(dx, x, size))) return SWCONV_EINVAL;
   const DropoutShape sh = shape_of(dtype, N, K, S);
-  if (dbias_dev && bp.parts > 1 && (!workspace_dev || workspace_bytes < bp.parts * K * (int64_t)sizeof(float))) return SWCONV_EINVAL;
+  if (dbias_dev && bp.parts > 1 &&
+      (!workspace_dev || workspace_bytes < bp.parts * K * (int64_t)sizeof(float)))
+    return SWCONV_EINVAL;
   float* partial = bp.parts > 1 ? (float*)workspace_dev : dbias_dev;
   const bool once = (relu ? 3 : 2) * N * K * S * size > kCacheBytes;
   const bool dense = sh.pad == 0 && dy_stride == K * S && dx_stride == K * S && (!relu || x_stride == K * S);
@@ -274,16 +278,18 @@ int swconv_dropout_backward(int dtype, int64_t N, int64_t K, int64_t S, const vo
     if (!dbias_dev) {
       const dim3 grid = item_grid<E>(sh);
       if (!relu)
-        return launch(dropout_kernel<E, Pass::backward, Bias::planes>, grid, kDropThreads, st, sh, rule, a, bias_dev, g, d, dense, once);
+        return launch(dropout_kernel<E, Pass::backward, Bias::planes>, grid, kDropThreads, st, sh, rule, a, bias_dev, g,
+                      d, dense, once);
       return dispatch_bias(S, K, [&](auto by) {
-        return launch(dropout_kernel<E, Pass::backward_relu, decltype(by)::value>, grid, kDropThreads, st, sh, rule, a, bias_dev, g, d, dense, once);
+        return launch(dropout_kernel<E, Pass::backward_relu, decltype(by)::value>, grid, kDropThreads, st, sh, rule, a,
+                      bias_dev, g, d, dense, once);
       });
     }
     if (S > 1) {
       const int64_t waves = kDropThreads / 64;
       const dim3 grid((unsigned)std::min<int64_t>(((int64_t)bp.units.units + waves - 1) / waves, kMaxGroups));
-      return launch(relu ? dropout_maps_grad_kernel<E, true> : dropout_maps_grad_kernel<E, false>, grid, kDropThreads, st, sh, bp.units, rule, a,
-                    bias_dev, g, d, partial, once);
+      auto kernel = relu ? dropout_maps_grad_kernel<E, true> : dropout_maps_grad_kernel<E, false>;
+      return launch(kernel, grid, kDropThreads, st, sh, bp.units, rule, a, bias_dev, g, d, partial, once);
     }
     const int64_t chunks = (K + 7) / 8 * kHalves<E>;  // of 16 bytes
     const int across_shift = std::min(8, ceil_log2(chunks));
@@ -291,11 +297,12 @@ int swconv_dropout_backward(int dtype, int64_t N, int64_t K, int64_t S, const vo
     auto kernel = !relu        ? dropout_features_grad_kernel<E, false, Bias::columns>
                   : K % 8 == 0 ? dropout_features_grad_kernel<E, true, Bias::columns>
                                : dropout_features_grad_kernel<E, true, Bias::ragged>;
-    return launch(kernel, grid, kDropThreads, st, sh, (uint32_t)N, across_shift, (uint32_t)bp.rows_per_chunk, rule, a, bias_dev, g, d, partial,
-                  once);
+    return launch(kernel, grid, kDropThreads, st, sh, (uint32_t)N, across_shift, (uint32_t)bp.rows_per_chunk, rule, a,
+                  bias_dev, g, d, partial, once);
   });
   if (rc || !dbias_dev || bp.parts == 1) return rc;
-  return launch(bias_grad_kernel, sum_grid, kBiasCols * kBiasDown, st, (const float*)partial, (uint32_t)bp.parts, (uint32_t)K, dbias_dev);
+  return launch(bias_grad_kernel, sum_grid, kBiasCols * kBiasDown, st, (const float*)partial, (uint32_t)bp.parts,
+                (uint32_t)K, dbias_dev);
 }
 
 int swconv_logprobs_workspace_bytes(int dtype, int64_t rows, int64_t classes, int top, int64_t* bytes) {
@@ -308,9 +315,10 @@ int swconv_logprobs_workspace_bytes(int dtype, int64_t rows, int64_t classes, in
   return SWCONV_OK;
 }
 
-int swconv_logprobs_forward(int dtype, int64_t rows, int64_t classes, const void* scores_dev, int64_t row_stride, const int32_t* labels_dev,
-                            int top, void* workspace_dev, int64_t workspace_bytes, void* hip_stream, float* logprob_dev,
-                            float* entropy_dev, float* stats_dev, int32_t* top_class_dev, float* top_logprob_dev) {
+int swconv_logprobs_forward(int dtype, int64_t rows, int64_t classes, const void* scores_dev, int64_t row_stride,
+                            const int32_t* labels_dev, int top, void* workspace_dev, int64_t workspace_bytes,
+                            void* hip_stream, float* logprob_dev, float* entropy_dev, float* stats_dev,
+                            int32_t* top_class_dev, float* top_logprob_dev) {
   if (int rc = check_scores(dtype, rows, classes, row_stride, &row_stride)) return rc;
   if (top < 0) return SWCONV_EINVAL;
   if (top > kTopMax) return SWCONV_EUNSUPPORTED;
@@ -323,7 +331,9 @@ int swconv_logprobs_forward(int dtype, int64_t rows, int64_t classes, const void
                         (const void*)top_class_dev, (const void*)top_logprob_dev})
     if ((uintptr_t)p % 4) return SWCONV_EINVAL;
   const Parts pt = parts_of(dtype, rows, classes, top);
-  if (pt.parts > 1 && (!workspace_dev || (uintptr_t)workspace_dev % 16 || workspace_bytes < parts_bytes(pt, rows, top))) return SWCONV_EINVAL;
+  if (pt.parts > 1 &&
+      (!workspace_dev || (uintptr_t)workspace_dev % 16 || workspace_bytes < parts_bytes(pt, rows, top)))
+    return SWCONV_EINVAL;
   auto* part_sums = (RowSums*)workspace_dev;
   auto* part_keys = (TopKey*)(part_sums + rows * pt.parts);
   const LogprobsOut out{logprob_dev, entropy_dev, stats_dev, top_class_dev, top_logprob_dev};
@@ -336,10 +346,10 @@ int swconv_logprobs_forward(int dtype, int64_t rows, int64_t classes, const void
     auto part = [&](auto waves, auto with_top, auto with_entropy) {
       constexpr int W = decltype(waves)::value;
       constexpr int kRows = W == 1 ? 4 : 1;  // parts of a workgroup
-      const int64_t groups = (rows * pt.parts + kRows - 1) / kRows;
-      return launch(logprobs_kernel<E, W, decltype(with_top)::value, decltype(with_entropy)::value>,
-                    dim3((unsigned)std::min(groups, kMaxGroups)), W == 1 ? 256 : W * 64, st, rows, classes, s, row_stride, labels_dev, top, pt.parts,
-                    pt.part_classes, once, out, part_sums, part_keys);
+      const dim3 grid((unsigned)std::min((rows * pt.parts + kRows - 1) / kRows, kMaxGroups));
+      return launch(logprobs_kernel<E, W, decltype(with_top)::value, decltype(with_entropy)::value>, grid,
+                    W == 1 ? 256 : W * 64, st, rows, classes, s, row_stride, labels_dev, top, pt.parts, pt.part_classes,
+                    once, out, part_sums, part_keys);
     };
     auto entropy = [&](auto waves, auto with_top) {
       return entropy_dev ? part(waves, with_top, std::true_type{}) : part(waves, with_top, std::false_type{});
@@ -350,14 +360,15 @@ int swconv_logprobs_forward(int dtype, int64_t rows, int64_t classes, const void
                    : pt.waves == 4 ? best(integral_constant<int, 4>{})
                                    : best(integral_constant<int, 16>{});
     if (rc || pt.parts == 1) return rc;
-    return launch(logprobs_join_kernel<E>, dim3((unsigned)std::min(rows, kMaxGroups)), 256, st, rows, classes, s, row_stride, labels_dev,
-                  top, pt.parts, out, (const RowSums*)part_sums, (const TopKey*)part_keys);
+    return launch(logprobs_join_kernel<E>, dim3((unsigned)std::min(rows, kMaxGroups)), 256, st, rows, classes, s,
+                  row_stride, labels_dev, top, pt.parts, out, (const RowSums*)part_sums, (const TopKey*)part_keys);
   });
 }
 
 int swconv_logprobs_backward(int dtype, int64_t rows, int64_t classes, const void* scores_dev, int64_t row_stride,
-                             const int32_t* labels_dev, const float* stats_dev, const float* entropy_dev, const float* dlogprob_dev,
-                             const float* dentropy_dev, void* hip_stream, void* dscores_dev, int64_t dscores_stride) {
+                             const int32_t* labels_dev, const float* stats_dev, const float* entropy_dev,
+                             const float* dlogprob_dev, const float* dentropy_dev, void* hip_stream, void* dscores_dev,
+                             int64_t dscores_stride) {
   if (int rc = check_scores(dtype, rows, classes, row_stride, &row_stride)) return rc;
   if (int rc = check_scores(dtype, rows, classes, dscores_stride, &dscores_stride)) return rc;
   if (rows == 0) return SWCONV_OK;
@@ -380,13 +391,17 @@ int swconv_logprobs_backward(int dtype, int64_t rows, int64_t classes, const voi
     const int64_t groups = (classes + kWordsElems<E> - 1) / kWordsElems<E>;
     auto grad = [&](auto with_entropy) {
       constexpr bool H = decltype(with_entropy)::value;
-      if (groups >= 128)
-        return launch(logprobs_grad_kernel<E, H>, dim3((unsigned)((groups + kGradThreads * kGradUnroll<E> - 1) / (kGradThreads * kGradUnroll<E>)), (unsigned)std::min<int64_t>(rows, 65535)),
-                      kGradThreads, st, rows, classes, s, row_stride, in, once, d, dscores_stride);
+      if (groups >= 128) {
+        constexpr int64_t kGroups = kGradThreads * kGradUnroll<E>;
+        const dim3 grid((unsigned)((groups + kGroups - 1) / kGroups), (unsigned)std::min<int64_t>(rows, 65535));
+        return launch(logprobs_grad_kernel<E, H>, grid, kGradThreads, st, rows, classes, s, row_stride, in, once, d,
+                      dscores_stride);
+      }
       const int shift = ceil_log2(groups);
       const int64_t down = kGradThreads >> shift;
-      return launch(logprobs_grad_short_kernel<E, H>, dim3((unsigned)std::min((rows + down - 1) / down, kMaxGroups)), kGradThreads, st, rows,
-                    classes, s, row_stride, in, shift, d, dscores_stride);
+      const dim3 grid((unsigned)std::min((rows + down - 1) / down, kMaxGroups));
+      return launch(logprobs_grad_short_kernel<E, H>, grid, kGradThreads, st, rows, classes, s, row_stride, in, shift, d,
+                    dscores_stride);
     };
     return dentropy_dev ? grad(std::true_type{}) : grad(std::false_type{});
   });

@@ -226,3 +226,44 @@ def test_more_rows_than_one_launch_has_workgroups_for():
     p1 = 1 / (1 + np.exp(-d.astype(np.float64)))
     want = np.where(np.arange(rows) % 2 == 1, 1 - p1, -p1)
     assert np.abs(dx[:, 1].double().cpu().numpy() - want).max() <= 2.0 ** -11 + 64 * U
+
+
+# (rows, classes, top): a wave, four and sixteen waves a row and rows in parts, with several tiles to a segment of the second
+# look; rows whose best classes overflow the common list (all scores equal in places)
+@pytest.mark.parametrize("name,rows,classes,top", [
+    ("f16", 1100, 34001, 8), ("bf16", 1100, 34001, 0), ("bf16", 300, 300007, 20), ("f32", 140, 600001, 64), ("bf16", 100, 2000003, 30),
+    ("f16", 3, 9000001, 64), ("bf16", 40000, 300, 64), ("f32", 5000, 4000, 33),
+])
+def test_large_rows_and_many(name, rows, classes, top):
+    dtype = TYPES[name][1]
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn((rows, classes), generator=gen, device="cuda").mul_(3).to(dtype)
+    x[rows // 2, ::2] = 11.0
+    x[-1, classes // 2:] = float("-inf")
+    labels = torch.randint(0, classes, (rows,), generator=gen, device="cuda").int()
+    xs = Rows.__new__(Rows)
+    xs.rows, xs.span, xs.stride, xs.view, xs.ptr = rows, classes, classes, x, x.data_ptr()
+    got = logprobs_forward(name, xs, labels, top)
+    step = max(1, (1 << 27) // classes)
+    for r in range(0, rows, step):
+        at = slice(r, min(rows, r + step))
+        z = x[at].double()
+        lp = torch.log_softmax(z, 1)
+        e = lambda a: torch.from_numpy(a[at]).cuda().double()
+        ls = torch.logsumexp(z - z.amax(1, keepdim=True), 1)
+        # additions one behind the other: classes / 64 + 32 at most; the scores lie within 40 of each other, or are masked
+        bound = U * (3 * 40 + 4 * (classes / 64 + 32) + 6 + 6 * np.log(classes)) + 2 * U * 60
+        assert ((e(got["stats"])[:, 1] - ls).abs() <= bound).all()
+        want = lp.gather(1, labels[at].long()[:, None])[:, 0]
+        seen = want > -np.inf
+        assert torch.equal(e(got["logprob"])[~seen], want[~seen])
+        assert ((e(got["logprob"]) - want)[seen].abs() <= bound).all()
+        if top:
+            value, index = torch.sort(z, dim=1, descending=True, stable=True)
+            value, index = value[:, :top], index[:, :top].int()
+            index[value == -np.inf] = -1
+            assert torch.equal(torch.from_numpy(got["top_class"][at]).cuda(), index)
+            wanted = lp.gather(1, index.long().clamp(min=0))
+            ok = index >= 0
+            assert ((e(got["top_logprob"]) - wanted)[ok].abs() <= bound).all()
+        del z, lp
