@@ -267,34 +267,25 @@ __device__ __forceinline__ K join_best(K best, K (*lds_keys)[N], int wave, int l
   return best;
 }
 
-// Where a lane's u-th group of a tile begins.  The groups that reach past the end of a row (or part) lie on its last V
-// elements instead, if it has V; what other groups hold of them counts as -inf.
-template <Elem E>
-__device__ __forceinline__ int64_t group_start(int64_t tile, int u, int64_t end, int lane) {
-  return min(tile + (u * 64 + lane) * kWordsElems<E>, max(end - kWordsElems<E>, (int64_t)0));
+// A tile's 16-byte groups of one lane.  Groups that reach past the end of a row (or part) lie on its last V elements
+// instead - so that every tile is read in one way, without the waits of several - and what other groups hold of these then
+// counts as -inf (cut_tile).  The row has V elements at least.
+template <Elem E, bool ONCE>
+__device__ __forceinline__ void load_tile(Words (&raw)[kLogpUnroll], const elem_t<E>* x_row, int64_t tile, int64_t end,
+                                          int lane) {
+  constexpr int V = kWordsElems<E>;
+  const int64_t last = end - V;
+#pragma unroll
+  for (int u = 0; u < kLogpUnroll; ++u)
+    raw[u] = load_words<E>(x_row + min(tile + (u * 64 + lane) * V, last), ONCE);
 }
 template <Elem E>
-__device__ __forceinline__ void load_tile(Words (&raw)[kLogpUnroll], const elem_t<E>* x_row, int64_t tile, int64_t end,
-                                          int lane, bool once) {
-  constexpr int V = kWordsElems<E>, U = kLogpUnroll;
-  if (tile + 64 * V * U <= end) {
-    const elem_t<E>* p = x_row + tile + lane * V;
-    if (once) {
+__device__ __forceinline__ void cut_tile(Words (&raw)[kLogpUnroll], int64_t tile, int64_t end, int lane) {
+  constexpr int V = kWordsElems<E>;
 #pragma unroll
-      for (int u = 0; u < U; ++u) raw[u] = load_words<E>(p + u * 64 * V, true);
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u) raw[u] = load_words<E>(p + u * 64 * V, false);
-    }
-  } else if (end >= V) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t j = group_start<E>(tile, u, end, lane);
-      raw[u] = without_first<E>(load_words<E>(x_row + j, false), (int)min(tile + (u * 64 + lane) * V - j, (int64_t)V));
-    }
-  } else {
-#pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = load_words_part<E>(x_row, u == 0 && lane == 0 ? (int)end : 0);
+  for (int u = 0; u < kLogpUnroll; ++u) {
+    const int64_t past = tile + (u * 64 + lane) * V - (end - V);
+    raw[u] = without_first<E>(raw[u], (int)max(min(past, (int64_t)V), (int64_t)0));
   }
 }
 
@@ -316,6 +307,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void logprobs_kernel
   __shared__ int waiting;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part_wave = wave % WAVES;
   constexpr int kPartsPerGroup = kWaves / WAVES;
+  // Four waves to a row ask for the next tile before they work on one: 4096 x 131072 without the best classes 191 -> 183 us,
+  // 64 x 150001 16.8 -> 16.0.  One wave to a row gains nothing (16384 x 8192 71 -> 78), sixteen lack the registers.
+  constexpr bool PREFETCH = WAVES == 4;
   const int64_t n_parts = rows * parts;
   for (int64_t group = blockIdx.x; group * kPartsPerGroup < n_parts; group += gridDim.x) {
     const int64_t id = group * kPartsPerGroup + wave / WAVES;
@@ -333,9 +327,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void logprobs_kernel
     float c = reference(a.m), seen_max = -INFINITY, lane_best = -INFINITY;
     int segment = 0, in_segment = 0;
     float n = 0.0f;  // scores equal to a.m in the whole wave
-    for (int64_t tile = first; tile < end; tile += kStep) {
-      Words raw[U];
-      load_tile<E>(raw, x_row, tile, end, lane, once);
+    auto see_tile = [&](const Words (&raw)[U], bool last) {
       float lane_max = word_elem<E>(raw[0], 0);
 #pragma unroll
       for (int k = 1; k < U * V; ++k) lane_max = __builtin_elementwise_maximum(lane_max, word_elem<E>(raw[k / V], k % V));
@@ -371,12 +363,40 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void logprobs_kernel
       if constexpr (TOP) {
         lane_best = fmaxf(lane_best, lane_max);
         seen_max = fmaxf(seen_max, lane_max);
-        if (++in_segment == segment_tiles || tile + kStep >= end) {
+        if (++in_segment == segment_tiles || last) {
           segment_max[wave][segment++][lane] = seen_max;
           seen_max = -INFINITY;
           in_segment = 0;
         }
       }
+    };
+    auto look_through = [&](auto once_or_not) {
+      constexpr bool ONCE = decltype(once_or_not)::value;
+      Words next[U];
+      if constexpr (PREFETCH) load_tile<E, ONCE>(next, x_row, first, end, lane);
+      for (int64_t tile = first; tile < end; tile += kStep) {
+        Words raw[U];
+        if constexpr (PREFETCH) {
+#pragma unroll
+          for (int u = 0; u < U; ++u) raw[u] = next[u];
+          load_tile<E, ONCE>(next, x_row, tile + kStep, end, lane);
+        } else {
+          load_tile<E, ONCE>(raw, x_row, tile, end, lane);
+        }
+        if (tile + kTile > end) cut_tile<E>(raw, tile, end, lane);
+        see_tile(raw, tile + kStep >= end);
+      }
+    };
+    if (end < V) {  // one wave's, one lane's
+      Words raw[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) raw[u] = load_words_part<E>(x_row, u == 0 && lane == 0 && first < end ? (int)end : 0);
+      see_tile(raw, true);
+    } else if (first < end) {
+      if (once)
+        look_through(std::true_type{});
+      else
+        look_through(std::false_type{});
     }
     const Label label = label_at<E>(wanted, x_row, classes);
     auto add = [](float x, float y) { return x + y; };
