@@ -150,7 +150,7 @@ BiasParts bias_parts(int64_t N, int64_t K, int64_t S) {
     const int64_t segments = (groups + kDropUnit - 1) / kDropUnit;
     // planes to a wave: what fills its steps of 64 items best, in 4096 waves at least if there is as much work (64 x 384
     // planes of 13 x 13 fp32: 23 planes to a wave 15.6 us, 5 planes 11.7; 4 x 384 planes 11.9 and 4.8).
-    const int64_t most = std::clamp<int64_t>(N * K * groups / 4096, groups, kDropUnit);
+    const int64_t most = std::clamp<int64_t>(N * K * groups / 4096, groups, std::max<int64_t>(groups, kDropUnit));
     int planes = 1;
     double best = 0;
     for (int p = 1; p <= 64 && p * groups <= most; ++p) {
