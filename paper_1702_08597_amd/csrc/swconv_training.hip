@@ -141,7 +141,6 @@ int rule_of(int64_t N, int relu, float p, const uint64_t* rng, uint64_t offset, 
 struct BiasParts {
   int64_t parts;
   MapUnits units{0, Divisor32(1), 0, 0, 1, 6};
-  int64_t rows_per_chunk = 1;
 };
 BiasParts bias_parts(int64_t N, int64_t K, int64_t S) {
   BiasParts b;
@@ -161,12 +160,10 @@ BiasParts bias_parts(int64_t N, int64_t K, int64_t S) {
                (uint32_t)N, planes, 6 - ceil_log2(planes)};
     b.parts = N * segments;
   } else {
-    // 1024 workgroups of the 16-bit types, of at least 4 rows a thread
-    const int64_t across = std::min<int64_t>(kDropThreads, (int64_t)1 << ceil_log2(groups)), down = kDropThreads / across;
-    const int64_t col_blocks = (groups + across - 1) / across;
-    const int64_t chunks = std::clamp<int64_t>((N + 4 * down - 1) / (4 * down), 1, std::max<int64_t>(1, 1024 / col_blocks));
-    b.rows_per_chunk = std::max<int64_t>(1, (N + chunks - 1) / chunks);
-    b.parts = (N + b.rows_per_chunk - 1) / b.rows_per_chunk;
+    // 1024 workgroups of the 16-bit types, each with its rows in flight at least
+    const int64_t across = std::min<int64_t>(kDropThreads, (int64_t)1 << ceil_log2(groups));
+    const int64_t col_blocks = (groups + across - 1) / across, down = kBiasRows * (kDropThreads / across);
+    b.parts = std::clamp<int64_t>((N + down - 1) / down, 1, std::max<int64_t>(1, 1024 / col_blocks));
   }
   return b;
 }
@@ -305,8 +302,8 @@ int swconv_dropout_backward(int dtype, int64_t N, int64_t K, int64_t S, const vo
     auto kernel = !relu        ? dropout_features_grad_kernel<E, false, Bias::columns>
                   : K % 8 == 0 ? dropout_features_grad_kernel<E, true, Bias::columns>
                                : dropout_features_grad_kernel<E, true, Bias::ragged>;
-    return launch(kernel, grid, kDropThreads, st, sh, (uint32_t)N, across_shift, (uint32_t)bp.rows_per_chunk, rule, a,
-                  bias_dev, g, d, partial, once);
+    return launch(kernel, grid, kDropThreads, st, sh, (uint32_t)N, across_shift, rule, a, bias_dev, g, d,
+                  partial, once);
   });
   if (rc || !dbias_dev || bp.parts == 1) return rc;
   return launch(bias_grad_kernel, sum_grid, kBiasCols * kBiasDown, st, (const float*)partial, (uint32_t)bp.parts,
