@@ -1,5 +1,5 @@
 """Dropout between layers and log probabilities at a network's end, from their definitions in 64 bits (numpy): the
-checker of swconv_dropout_* and swconv_logprobs_*."""
+oracle of swconv_dropout_* and swconv_logprobs_*."""
 from __future__ import annotations
 
 import numpy as np

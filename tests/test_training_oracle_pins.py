@@ -1,4 +1,4 @@
-"""Pins of the checker of dropout and log probabilities: the generator against its published vectors and by its
+"""Pins of the oracle of dropout and log probabilities: the generator against its published vectors and by its
 statistics, gradients against differences, the definitions on rows that can be written down."""
 import numpy as np
 import pytest
