@@ -66,10 +66,11 @@ int dispatch_type(int dtype, F&& f) {
 }
 
 template <typename F>
-int dispatch_bias(int64_t S, int64_t K, F&& f) {
+int dispatch_bias(int64_t S, int64_t K, const float* bias, F&& f) {
   using std::integral_constant;
   if (S > 1) return f(integral_constant<Bias, Bias::planes>{});
-  return K % 8 == 0 ? f(integral_constant<Bias, Bias::columns>{}) : f(integral_constant<Bias, Bias::ragged>{});
+  if (!bias || K % 8 == 0) return f(integral_constant<Bias, Bias::columns>{});  // none: 8 zeros for all
+  return K > 8 ? f(integral_constant<Bias, Bias::ragged>{}) : f(integral_constant<Bias, Bias::elements>{});
 }
 
 // Rows of `span` elements, `stride` apart.
@@ -230,7 +231,7 @@ int swconv_dropout_forward(int dtype, int64_t N, int64_t K, int64_t S, const voi
   return dispatch_type(dtype, [&](auto e) {
     constexpr Elem E = decltype(e)::value;
     const dim3 grid = item_grid<E>(sh);
-    return dispatch_bias(S, K, [&](auto by) {
+    return dispatch_bias(S, K, bias_dev, [&](auto by) {
       return launch(dropout_kernel<E, Pass::forward, decltype(by)::value>, grid, kDropThreads, st, sh, rule,
                     images<E>(x), bias_dev, Images<E>{}, images<E>(y), dense, once);
     });
@@ -285,7 +286,7 @@ int swconv_dropout_backward(int dtype, int64_t N, int64_t K, int64_t S, const vo
       if (!relu)
         return launch(dropout_kernel<E, Pass::backward, Bias::planes>, grid, kDropThreads, st, sh, rule, a, bias_dev, g,
                       d, dense, once);
-      return dispatch_bias(S, K, [&](auto by) {
+      return dispatch_bias(S, K, bias_dev, [&](auto by) {
         return launch(dropout_kernel<E, Pass::backward_relu, decltype(by)::value>, grid, kDropThreads, st, sh, rule, a,
                       bias_dev, g, d, dense, once);
       });
@@ -299,9 +300,9 @@ int swconv_dropout_backward(int dtype, int64_t N, int64_t K, int64_t S, const vo
     const int64_t chunks = (K + 7) / 8 * kHalves<E>;  // of 16 bytes
     const int across_shift = std::min(8, ceil_log2(chunks));
     const dim3 grid((unsigned)((chunks + (1 << across_shift) - 1) >> across_shift), (unsigned)bp.parts);
-    auto kernel = !relu        ? dropout_features_grad_kernel<E, false, Bias::columns>
-                  : K % 8 == 0 ? dropout_features_grad_kernel<E, true, Bias::columns>
-                               : dropout_features_grad_kernel<E, true, Bias::ragged>;
+    auto kernel = !relu                     ? dropout_features_grad_kernel<E, false, Bias::columns>
+                  : !bias_dev || K % 8 == 0 ? dropout_features_grad_kernel<E, true, Bias::columns>
+                                            : dropout_features_grad_kernel<E, true, Bias::elements>;
     return launch(kernel, grid, kDropThreads, st, sh, (uint32_t)N, across_shift, rule, a, bias_dev, g, d,
                   partial, once);
   });

@@ -9,7 +9,8 @@ from paper_1702_08597_amd import binding as sw
 from test_gpu_dropout import check as check_dropout
 from test_gpu_logprobs import check as check_logprobs
 from test_gpu_logprobs import scores
-from training_ops import TYPES, Rows, dropout_backward, dropout_forward, guarded, logprobs_backward, logprobs_forward, ptr, rng_state, stream
+from training_ops import (TYPES, Rows, dbias_bound, dropout_backward, dropout_bound, dropout_forward, guarded, logprobs_backward,
+                          logprobs_forward, ptr, rng_state, stream)
 
 pytestmark = pytest.mark.gpu
 
@@ -129,3 +130,31 @@ def test_small_values_are_kept():
     y = Rows("f32", 1, 4)
     dropout_forward("f32", x, 1, 4, 1, None, 0, 0.0, None, 0, y)
     assert torch.equal(y.view, x.view)
+
+
+@pytest.mark.parametrize("name", list(TYPES))
+@pytest.mark.parametrize("K", [7, 9, 10, 11, 12, 13, 14, 15, 257, 260, 263])
+def test_bias_of_ragged_rows(name, K):
+    """The bias lies between NaN and off 16 bytes; every count of columns behind the last whole chunk."""
+    N, p, relu = 37, 0.2, 1
+    rng = np.random.default_rng(K)
+    around = torch.full((K + 18,), float("nan"), device="cuda")
+    b = around[9:9 + K]
+    b.copy_(torch.from_numpy(rng.standard_normal(K).astype(np.float32)))
+    b64 = b.double().cpu().numpy()
+    x = Rows(name, N, K, values=rng.standard_normal((N, K)).astype(np.float32))
+    dy = Rows(name, N, K, values=rng.standard_normal((N, K)).astype(np.float32))
+    y, dx, dx2, db = Rows(name, N, K), Rows(name, N, K), Rows(name, N, K), guarded(K)
+    state = rng_state(11, 2)
+    dropout_forward(name, x, N, K, 1, b, relu, p, state, 4, y)
+    dropout_backward(name, dy, x, N, K, 1, b, relu, p, state, 4, dx, db)
+    dropout_backward(name, dy, x, N, K, 1, b, relu, p, state, 4, dx2, None)
+    x64, dy64 = x.f64().reshape(N, K, 1), dy.f64().reshape(N, K, 1)
+    want = ref.dropout_forward(x64, b64, relu, p, 11, 6)
+    assert (np.abs(y.f64().reshape(N, K, 1) - want) <= dropout_bound(name, want, 3)).all()
+    wdx, wdb = ref.dropout_backward(dy64, x64, b64, relu, p, 11, 6)
+    for got in (dx, dx2):
+        assert (np.abs(got.f64().reshape(N, K, 1) - wdx) <= dropout_bound(name, wdx, 2)).all()
+        assert got.guards_hold()
+    assert (np.abs(db[:K].double().cpu().numpy() - wdb) <= dbias_bound(wdx)).all()
+    assert y.guards_hold()
