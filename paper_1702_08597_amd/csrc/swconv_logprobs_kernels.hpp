@@ -346,7 +346,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void logprobs_kernel
     float c = reference(a.m), seen_max = -INFINITY, lane_best = -INFINITY;
     int segment = 0, in_segment = 0;
     float n = 0.0f;  // scores equal to a.m in the whole wave
-    float s_low = 0.0f, t_low = 0.0f;
+    float n_low = 0.0f, s_low = 0.0f, t_low = 0.0f;
     auto see_tile = [&](const Words (&raw)[U], bool last) {
       float lane_max = word_elem<E>(raw[0], 0);
 #pragma unroll
@@ -368,7 +368,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void logprobs_kernel
           a = raised(a, m);
           c = reference(m);
           n = 0.0f;
-          s_low = t_low = 0.0f;
+          n_low = s_low = t_low = 0.0f;
         }
         int equal = 0;
 #pragma unroll
@@ -380,7 +380,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void logprobs_kernel
           s.add(k, 1.0f, e);
           if constexpr (ENTROPY) t.add(k, d, e);
         }
-        n += (float)equal;
+        add_exactly(n, n_low, (float)equal);
       }
       add_exactly(a.s, s_low, s.total);
       if constexpr (ENTROPY) add_exactly(a.t, t_low, t.total);

@@ -69,3 +69,21 @@ def test_scores_that_rise_all_along_a_row(name, rows, classes, top):
     ls_bound, H_bound = sum_bounds(ls, mean_d, mean_d, changes)
     assert (np.abs(got["stats"][:, 1] - ls) <= ls_bound).all()
     assert (np.abs(got["entropy"] - (ls + mean_d)) <= H_bound).all()
+
+
+def test_more_equal_scores_than_fp32_counts():
+    """More than 2^24 equal scores in one wave, an odd number of them in every tile."""
+    rows, classes = 257, 5 << 24
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 43 GB")
+    x = torch.zeros((rows, classes), dtype=torch.float16, device="cuda")
+    x[:, ::2048] = -1.0
+    got = logprobs_forward("f16", rows_of(x), None, 0)
+    others = classes // 2048
+    n, s = classes - others, others * np.exp(-1.0)
+    ls, mean_d = np.log(n + s), s / (n + s)
+    ls_bound, H_bound = sum_bounds(ls, mean_d, 0.0, 1)
+    assert (np.abs(got["stats"][:, 1] - ls) <= ls_bound).all()
+    assert (np.abs(got["entropy"] - (ls + mean_d)) <= H_bound).all()
+    del x
+    torch.cuda.empty_cache()
