@@ -1,5 +1,5 @@
-"""The sums of swconv_logprobs_forward in long rows: bounds that do not grow with the row, and rows whose scores are all rounded
-the same way.
+"""The sums of swconv_logprobs_forward in long rows: bounds that do not grow with the row, rows whose scores are all rounded the
+same way, and rows of which every part, wave and tail has to be there.
 
 U is half a step of fp32.  A term exp(x - m) is off by 2 U |x - m| (the exponent's rounding, and that of log2 e) and 2 U (the
 instruction) of itself.  All terms are of one sign, so an addition is off by U of the sum at most: 7 in a group of 16 bytes, 3 to
@@ -10,7 +10,7 @@ import numpy as np
 import pytest
 import torch
 
-from training_ops import TYPES, U, Rows, logprobs_forward
+from training_ops import TYPES, U, Rows, half_step, logprobs_backward, logprobs_forward
 
 pytestmark = pytest.mark.gpu
 
@@ -69,6 +69,72 @@ def test_scores_that_rise_all_along_a_row(name, rows, classes, top):
     ls_bound, H_bound = sum_bounds(ls, mean_d, mean_d, changes)
     assert (np.abs(got["stats"][:, 1] - ls) <= ls_bound).all()
     assert (np.abs(got["entropy"] - (ls + mean_d)) <= H_bound).all()
+
+
+@pytest.mark.parametrize("name", list(TYPES))
+@pytest.mark.parametrize("rows,classes,top", [(64, 150001, 20), (64, 300007, 0), (40, 1000003, 5), (200, 262147, 3), (300, 262147, 3),
+                                              (2048, 65537, 1), (2048, 65537, 0), (64, 40001, 5)])
+def test_every_stretch_of_a_row_counts(name, rows, classes, top):
+    """Row i holds equal scores in the i-th stretch of its classes alone, the others are masked or far below: ls is the logarithm of
+    their number, to the last digits; the last rows have theirs at the very end."""
+    x = torch.full((rows, classes), float("-inf"), dtype=TYPES[name][1], device="cuda")
+    x[::2] = -1000.0
+    ends = [(i * classes // rows, max((i + 1) * classes // rows, i * classes // rows + 1)) for i in range(rows)]
+    ends[-3:] = [(classes - 1, classes), (classes - 2, classes), (classes - 9, classes)]
+    for i, (a, b) in enumerate(ends):
+        x[i, a:b] = 0.5
+    got = logprobs_forward(name, rows_of(x), torch.tensor([a for a, _ in ends], device="cuda").int(), top)
+    n = np.array([b - a for a, b in ends])
+    # counted, not added: the logarithm and nothing else
+    for value, want in ((got["stats"][:, 1], np.log(n)), (got["entropy"], np.log(n)), (got["logprob"], -np.log(n))):
+        assert (np.abs(value - want) <= 4 * U * np.log(n)).all()
+    assert (got["stats"][:, 0] == 0.5).all()
+    for i in range(rows):
+        left = min(top, n[i])
+        np.testing.assert_array_equal(got["top_class"][i, :left], ends[i][0] + np.arange(left))
+
+
+@pytest.mark.parametrize("name,rows,classes,top", [
+    ("f16", 1100, 34001, 8), ("bf16", 2100, 65537, 0), ("bf16", 300, 300007, 20), ("f32", 140, 600001, 64), ("bf16", 100, 2000003, 30),
+    ("f16", 3, 9000001, 64), ("f32", 5000, 4000, 33),
+])
+def test_values_and_gradients_of_large_rows(name, rows, classes, top):
+    gen = torch.Generator(device="cuda").manual_seed(classes)
+    x = torch.randn((rows, classes), generator=gen, device="cuda").mul_(2).to(TYPES[name][1])
+    x[-1, classes // 2:] = float("-inf")
+    labels = torch.randint(0, classes // 2, (rows,), generator=gen, device="cuda").int()
+    g, h = torch.randn(rows, generator=gen, device="cuda"), torch.randn(rows, generator=gen, device="cuda")
+    xs = rows_of(x)
+    got = logprobs_forward(name, xs, labels, top)
+    dx = torch.full_like(x, 77.0)
+    logprobs_backward(name, xs, labels, got, g, h, rows_of(dx))
+    rel, tiny = half_step(name)
+    step = max(1, (1 << 25) // classes)
+    for r in range(0, rows, step):
+        at = slice(r, min(rows, r + step))
+        z = x[at].double()
+        d = z - z.amax(1, keepdim=True)
+        ls = torch.logsumexp(d, 1)
+        lp = d - ls[:, None]
+        p = lp.exp()
+        lp0 = torch.where(p > 0, lp, torch.zeros_like(lp))
+        mean_d = -(p * torch.where(p > 0, d, torch.zeros_like(d))).sum(1)
+        H = ls + mean_d
+        # scores drawn independently: the k-th tile changes the largest one with chance 1 / k, so 24 changes and 22 joins
+        # are more than there are; the terms that count lie within 30
+        ls_bound, H_bound = sum_bounds(ls, mean_d, 30.0, 46)
+        e = lambda a: torch.from_numpy(a[at]).cuda().double()
+        assert ((e(got["stats"])[:, 1] - ls).abs() <= ls_bound).all()
+        assert ((e(got["entropy"]) - H).abs() <= H_bound).all()
+        own = lp.gather(1, labels[at].long()[:, None])
+        assert ((e(got["logprob"]) - own[:, 0]).abs() <= ls_bound + 2 * U * (2 * own[:, 0].abs() + ls)).all()
+        g64, h64 = g[at].double()[:, None], h[at].double()[:, None]
+        want = -p * (g64 + h64 * (lp0 + H[:, None]))
+        want.scatter_add_(1, labels[at].long()[:, None], g64)
+        elp = ls_bound[:, None] + 4 * U * (lp0.abs() + ls[:, None])
+        factor = g64.abs() + h64.abs() * (lp0.abs() + H[:, None])
+        err = p * factor * (elp + 3 * U * lp0.abs() + 8 * U) + p * h64.abs() * (elp + H_bound[:, None]) + 2 * U * g64.abs()
+        assert ((dx[at].double() - want).abs() <= err * 1.01 + want.abs() * rel + 1e-37 + tiny).all()
 
 
 def test_more_equal_scores_than_fp32_counts():
