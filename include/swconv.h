@@ -423,7 +423,7 @@ int swconv_dropout_workspace_bytes(int64_t N, int64_t K, int64_t S, int64_t* byt
  * Sums are fp32.  A score of -inf is masked: it has probability 0 and is never among the best; places that no class is left
  * for hold -1 and -inf.  A row without any unmasked class has m = -inf, ls = 0, log p = -inf and entropy 0.  The types'
  * lowest finite values are scores like others.  A row that holds NaN or +inf gives NaN for every float and -1
- * for every class; a label >= classes gives NaN (and reads nothing).
+ * for every class, but for logprob_dev, which stays 0 where there is no label; a label >= classes gives NaN (and reads nothing).
  * Errors: EINVAL (unknown dtype, rows < 0, classes < 1, top < 0, a stride below `classes`, null or misaligned pointers,
  * no output, a workspace that is too small), EUNSUPPORTED (sizes beyond these, top > 64), EHIP.
  */
