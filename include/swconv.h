@@ -363,8 +363,10 @@ typedef enum {
  *               rate).  0: nothing is dropped and rng_dev is not read; 1: y = 0.
  *   rng_dev     DEVICE, two 64-bit words: the seed and a step count, read when the kernel runs - a captured graph
  *               makes new masks when the caller's program changes them between replays.
- *   offset      added to the step count (mod 2^64), e.g. the number of the layer.  Calls of equal seed and step + offset
- *               and equal shape make equal masks.
+ *   offset      added to the step count (mod 2^64).  The mask depends on that sum: calls of equal seed and step + offset make
+ *               equal decisions at the rows and columns that they have in common, whatever their sizes.  So a network of L
+ *               dropout layers gives them the offsets 0 .. L - 1 and counts the step up by L for each pass (counted up by 1,
+ *               a layer would have the mask that the next one had a pass earlier), or has a state of its own for each layer.
  *   y_dev       DEVICE, N x K x S with y_stride; may be x_dev with the same stride, else shares no element with x.
  *               What lies between the images is not written, and what it holds does not matter.
  * The mask is a function of the sizes and the four numbers alone, whatever dtype, strides and launch: with
