@@ -360,12 +360,14 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutShape sh, 
   for (uint64_t first = wave * kTurn; first < sh.items; first += gridDim.x * (kTurn * kWaves)) {
     const uint32_t left = (uint32_t)min(sh.items - first, kTurn);
     Place at[COUNT];
-    if (dense) {
-      if (once)
-        dropout_turn<E, PASS, B, Read::once, true>(sh, rule, x, bias, dy, out, first, left, at, lane);
-      else
-        dropout_turn<E, PASS, B, Read::whole, true>(sh, rule, x, bias, dy, out, first, left, at, lane);
-      continue;
+    if constexpr (B == Bias::planes || B == Bias::columns) {  // the other two are for rows that end inside an item
+      if (dense) {
+        if (once)
+          dropout_turn<E, PASS, B, Read::once, true>(sh, rule, x, bias, dy, out, first, left, at, lane);
+        else
+          dropout_turn<E, PASS, B, Read::whole, true>(sh, rule, x, bias, dy, out, first, left, at, lane);
+        continue;
+      }
     }
     turn_places<E>(sh, first, lane, at);
     bool whole = sh.items - first - left >= 8;  // 8 elements at least lie behind
