@@ -192,7 +192,7 @@ __device__ __forceinline__ int chunk_size(const DropoutShape& sh, uint32_t col) 
   return (int)min((int64_t)sh.cols - col, (int64_t)kChunk<E>);
 }
 // The bias by channels of maps, by columns of features, by columns that fill no item at the end of a row: there the bias's
-// last V are read for its last chunk, and shift_bias moves them; rows of less than a chunk and kernels that read their bias
+// last V are read for its last chunk, and shift_biases moves them; rows of less than a chunk and kernels that read their bias
 // once take it by the element (7416 x 8603 fp16 by the element 142 us, so 60.6).  None: zeros.
 enum class Bias { planes, columns, ragged, elements };
 __device__ const float kNoBias[8] = {};
@@ -224,21 +224,11 @@ __device__ __forceinline__ void load_bias(const DropoutShape& sh, const BiasAt& 
   }
 }
 
-// The bias of a chunk of n columns from that of a row's last V, n of which are its own; few waves have such chunks.  fp32 looks at
-// each (3708 x 8603 47 us, all of a turn's at once 53), the 16-bit types at all at once, with the moves written out on the
-// turn's array (7416 x 8603 fp16 60.6 us in 40 registers; chunk by chunk 67, through the fp32 form's moves 77, in 52).
-template <Elem E>
-__device__ __forceinline__ void shift_bias(int n, float (&b)[kChunk<E>]) {
-  constexpr int V = kChunk<E>;
-  if (__ballot(n > 0 && n < V) == 0) return;
-  const int by = n > 0 ? V - n : 0;
-#pragma unroll
-  for (int step = V / 2; step; step /= 2)
-#pragma unroll
-    for (int i = 0; i + step < V; ++i) b[i] = by & step ? b[i + step] : b[i];
-}
+// The biases of chunks of n columns each from those of a row's last V, n of which are their own; few waves have such chunks.
+// fp32 looks at each chunk for itself (3708 x 8603 47 us, at all of a turn at once 53), the 16-bit types at all at once (7416 x
+// 8603 fp16 60.6 us in 40 registers; chunk by chunk 67).
 template <Elem E, int COUNT>
-__device__ __forceinline__ void shift_biases(const int (&n)[COUNT], float (&b)[COUNT][kChunk<E>]) {
+__device__ __forceinline__ void shift_biases(const int* n, float (*b)[kChunk<E>]) {
   constexpr int V = kChunk<E>;
   bool any = false;
 #pragma unroll
@@ -333,14 +323,14 @@ __device__ __forceinline__ void dropout_turn(const DropoutShape& sh, const Dropo
 #pragma unroll
     for (int s = 0; s < kDropSteps<E>; ++s) chunk_words<E>(g, at[s * H], at[s * H + H - 1], lane, w[s]);
   constexpr bool kShift = B == Bias::ragged && PASS != Pass::backward;
-  if constexpr (kShift && H == 1) shift_biases<E>(n, b);
+  if constexpr (kShift && H == 1) shift_biases<E, COUNT>(n, b);
 #pragma unroll
   for (int s = 0; s < kDropSteps<E>; ++s) {
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       const int c = s * H + h;
       float v[V];
-      if constexpr (kShift && H == 2) shift_bias<E>(n[c], b[c]);
+      if constexpr (kShift && H == 2) shift_biases<E, 1>(n + c, b + c);
       if constexpr (PASS == Pass::forward)
         forward_chunk<E>(rule, in[c], b[c], w[s][h], v);
       else
