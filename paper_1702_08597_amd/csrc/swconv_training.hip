@@ -179,21 +179,28 @@ int check_scores(int dtype, int64_t rows, int64_t classes, int64_t given, int64_
   return rows > kMost || *stride > kMost || (rows > 1 && rows - 1 > kMost / *stride) ? SWCONV_EUNSUPPORTED : SWCONV_OK;
 }
 
-// How many waves share a row, and into how many parts it is cut.  A tile is what a wave reads at a time (8 KB of fp32, 4 of
-// the 16-bit types).  Times of bf16 rows with the best 5, in us:
-//   a wave per row where rows alone fill the chip (1024 SIMDs) and are short enough for their number: 2048 x 20000 30
-//   (four waves 39), 1024 x 131072 92 (71); past 8 tiles for up to 8 best classes only (4096 x 131072 with the best 20: 243, four
-//   waves 216, whose bar is that of more lanes); and rows of one or two tiles in any case;
-//   four waves of a workgroup, sixteen for long rows that leave CUs idle: 256 x 131072 24 (four waves 31);
-//   parts of at least 6 tiles and a second launch for few rows, up to two workgroups a CU: 1 x 131072 13 (one workgroup 18.5),
-//   64 x 131072 17 (21); from 64 rows on parts of 16 tiles, past 128 rows none: 256 x 131072 in two parts 35 (24).
+// How many waves share a row, and into how many parts it is cut.  A tile is what a wave reads at a time, 4 KB.  Times of bf16
+// rows with entropies and the best class in us, inputs from memory:
+//   a wave per row where rows alone fill the chip, 7 to a CU: 131072 classes of 1536 rows 118 (four waves 104), 1792 123
+//   (128), 4096 235 (268), and alike from 14 tiles on; shorter rows, of which four waves get few tiles each, from 128 rows to a
+//   tile on, 4 to a CU at least: 16384 classes of 768 rows 20 (15), 1024 20 (20), 1536 23 (25).  Past 32 tiles not with more than 8
+//   best classes (131072 classes of 2048 rows with the best 20 160, four waves 147, whose bar is that of more lanes; 65536
+//   classes 82 and 82) and not of fp32 (131072 classes of 2048 rows with the best 8 222, four waves 218; 32768 classes of 4096
+//   rows with the best 112 and 119); rows of one or two tiles in any case;
+//   four waves of a workgroup, sixteen for rows of 12 tiles at least while a CU has only one of them: 131072 classes of 256
+//   rows 24 (four waves 26), 257 rows 36 (30); 24576 classes 10 (11) and 17 (12);
+//   parts of at least 6 tiles and a second launch for few rows, up to two workgroups a CU, here with the best 5: 1 x 131072 13
+//   (one workgroup 18), 64 x 131072 18 (20); from 64 rows on parts of 16 tiles, past 128 rows none: 256 x 131072 in two parts
+//   27 (23).
 struct Parts {
   int waves, parts;
   int64_t part_classes;
 };
 Parts parts_of(int dtype, int64_t rows, int64_t classes, int top) {
   const int64_t tile = 64 * (16 / size_of(dtype)) * kLogpUnroll, tiles = (classes + tile - 1) / tile;
-  if (tiles <= 2 || (rows >= 1024 && tiles * (top ? 64 : 96) <= rows && (tiles <= 8 || top <= 8))) return {1, 1, classes};
+  const bool shared_when_long = top > 8 || dtype == SWCONV_F32;
+  if (tiles <= 2 || (rows >= std::clamp<int64_t>(128 * tiles, 1024, 1792) && (tiles <= 32 || !shared_when_long)))
+    return {1, 1, classes};
   if (rows > 256 || tiles < 12) return {4, 1, classes};
   int64_t parts = 1;
   if (rows > 0 && rows <= 128)
