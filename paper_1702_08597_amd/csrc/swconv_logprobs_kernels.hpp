@@ -324,7 +324,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void logprobs_kernel
   __shared__ uint16_t owners[TOP ? kWaves : 1][kWaiting];
   __shared__ float bars[kWaves];
   __shared__ int waiting;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part_wave = wave % WAVES;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part_wave = wave % WAVES;
   constexpr int kPartsPerGroup = kWaves / WAVES;
   // Four waves to a row ask for the next tile before they work on one: 4096 x 131072 without the best classes 191 -> 183 us,
   // 64 x 150001 16.8 -> 16.0.  One wave to a row gains nothing (16384 x 8192 71 -> 78), sixteen lack the registers.
