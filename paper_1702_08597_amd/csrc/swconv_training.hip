@@ -179,16 +179,18 @@ int check_scores(int dtype, int64_t rows, int64_t classes, int64_t given, int64_
   return rows > kMost || *stride > kMost || (rows > 1 && rows - 1 > kMost / *stride) ? SWCONV_EUNSUPPORTED : SWCONV_OK;
 }
 
-// How many waves share a row, and into how many parts it is cut.  A tile is what a wave reads at a time, 4 KB.  Times of bf16
-// rows with entropies and the best class in us, inputs from memory:
-//   a wave per row where rows alone fill the chip, 7 to a CU: 131072 classes of 1536 rows 118 (four waves 104), 1792 123
-//   (128), 4096 235 (268), and alike from 14 tiles on; shorter rows, of which four waves get few tiles each, from 128 rows to a
-//   tile on, 4 to a CU at least: 16384 classes of 768 rows 20 (15), 1024 20 (20), 1536 23 (25).  Past 32 tiles not with more than 8
-//   best classes (131072 classes of 2048 rows with the best 20 160, four waves 147, whose bar is that of more lanes; 65536
-//   classes 82 and 82) and not of fp32 (131072 classes of 2048 rows with the best 8 222, four waves 218; 32768 classes of 4096
-//   rows with the best 112 and 119); rows of one or two tiles in any case;
+// How many waves share a row, and into how many parts it is cut.  A tile is what a wave reads at a time, 4 KB; aligned: every
+// row begins on 16 bytes.  Times of bf16 rows with entropies and the best class in us, inputs from memory:
+//   a wave per row where rows alone fill the chip, 7 to a CU (32768 classes of 1536 rows 35, four waves 31; of 1792 36 and 37,
+//   of 4096 64 and 74), for short rows, of which four waves get few tiles each, from 160 rows to a tile on (256 without best
+//   classes, whose second look costs four waves more), 4 to a CU at least (5): 16384 classes of 1024 rows 20 and 19, of 1280 22
+//   and 21, of 1536 22 and 23.  Up to 24 tiles: 49152 classes of 4096 rows 86 and 95, 131072 of them 228 and 221, fp32 24576
+//   classes 82 and 85, 65536 classes 222 and 208; up to 10 without best classes: 20480 classes of 4096 rows 37 and 41, 32768 60
+//   and 54.  16-bit rows that are not aligned, which four waves read more slowly (131035 classes of 4096 rows 231 and 263), at any
+//   length, with more than 8 best classes up to 32 tiles (2048 rows with the best 20: 65499 classes 80 and 81, 131035 classes
+//   158 and 144).  Rows of one or two tiles in any case;
 //   four waves of a workgroup, sixteen for rows of 12 tiles at least while a CU has only one of them: 131072 classes of 256
-//   rows 24 (four waves 26), 257 rows 36 (30); 24576 classes 10 (11) and 17 (12);
+//   rows 22 (four waves 25), 257 rows 35 (28); 24576 classes 10 (11) and 17 (12);
 //   parts of at least 6 tiles and a second launch for few rows, up to two workgroups a CU, here with the best 5: 1 x 131072 13
 //   (one workgroup 18), 64 x 131072 18 (20); from 64 rows on parts of 16 tiles, past 128 rows none: 256 x 131072 in two parts
 //   27 (23).
@@ -196,11 +198,11 @@ struct Parts {
   int waves, parts;
   int64_t part_classes;
 };
-Parts parts_of(int dtype, int64_t rows, int64_t classes, int top) {
+Parts parts_of(int dtype, int64_t rows, int64_t classes, int top, bool aligned) {
   const int64_t tile = 64 * (16 / size_of(dtype)) * kLogpUnroll, tiles = (classes + tile - 1) / tile;
-  const bool shared_when_long = top > 8 || dtype == SWCONV_F32;
-  if (tiles <= 2 || (rows >= std::clamp<int64_t>(128 * tiles, 1024, 1792) && (tiles <= 32 || !shared_when_long)))
-    return {1, 1, classes};
+  const int64_t filled = top ? std::clamp<int64_t>(160 * tiles, 1024, 1792) : std::clamp<int64_t>(256 * tiles, 1280, 1792);
+  const int64_t longest = aligned || dtype == SWCONV_F32 ? (top ? 24 : 10) : top > 8 ? 32 : tiles;
+  if (tiles <= 2 || (rows >= filled && tiles <= longest)) return {1, 1, classes};
   if (rows > 256 || tiles < 12) return {4, 1, classes};
   int64_t parts = 1;
   if (rows > 0 && rows <= 128)
@@ -324,7 +326,7 @@ int swconv_logprobs_workspace_bytes(int dtype, int64_t rows, int64_t classes, in
   if (int rc = check_scores(dtype, rows, classes, 0, &stride)) return rc;
   if (top < 0) return SWCONV_EINVAL;
   if (top > kTopMax) return SWCONV_EUNSUPPORTED;
-  *bytes = parts_bytes(parts_of(dtype, rows, classes, top), rows, top);
+  *bytes = parts_bytes(parts_of(dtype, rows, classes, top, true), rows, top);  // parts are of few rows, aligned or not
   return SWCONV_OK;
 }
 
@@ -336,14 +338,16 @@ int swconv_logprobs_forward(int dtype, int64_t rows, int64_t classes, const void
   if (top < 0) return SWCONV_EINVAL;
   if (top > kTopMax) return SWCONV_EUNSUPPORTED;
   if (rows == 0) return SWCONV_OK;
+  const int64_t size = size_of(dtype);
   const Rows x{scores_dev, rows, classes, row_stride};
-  if (!placed(x, size_of(dtype)) || (logprob_dev && !labels_dev) || (top > 0) != (top_class_dev && top_logprob_dev) ||
+  if (!placed(x, size) || (logprob_dev && !labels_dev) || (top > 0) != (top_class_dev && top_logprob_dev) ||
       (!logprob_dev && !entropy_dev && !stats_dev && !top))
     return SWCONV_EINVAL;
   for (const void* p : {(const void*)labels_dev, (const void*)logprob_dev, (const void*)entropy_dev, (const void*)stats_dev,
                         (const void*)top_class_dev, (const void*)top_logprob_dev})
     if ((uintptr_t)p % 4) return SWCONV_EINVAL;
-  const Parts pt = parts_of(dtype, rows, classes, top);
+  const bool aligned = (uintptr_t)scores_dev % 16 == 0 && (rows == 1 || row_stride * size % 16 == 0);
+  const Parts pt = parts_of(dtype, rows, classes, top, aligned);
   if (pt.parts > 1 &&
       (!workspace_dev || (uintptr_t)workspace_dev % 16 || workspace_bytes < parts_bytes(pt, rows, top)))
     return SWCONV_EINVAL;
@@ -352,7 +356,7 @@ int swconv_logprobs_forward(int dtype, int64_t rows, int64_t classes, const void
   const LogprobsOut out{logprob_dev, entropy_dev, stats_dev, top_class_dev, top_logprob_dev};
   const hipStream_t st = (hipStream_t)hip_stream;
   const StreamDevice device(st);
-  const bool once = rows * classes * size_of(dtype) > kCacheBytes;
+  const bool once = rows * classes * size > kCacheBytes;
   return dispatch_type(dtype, [&](auto e) {
     constexpr Elem E = decltype(e)::value;
     const auto* s = (const elem_t<E>*)scores_dev;

@@ -31,7 +31,8 @@ def sum_bounds(ls, mean_d, reach, changes):
 
 # one wave, four and sixteen waves to a row, and rows in parts
 SHAPES = [("bf16", 2048, 65536, 1), ("f16", 8192, 262144, 1), ("f32", 4096, 65536, 3), ("bf16", 300, 262144, 5), ("f16", 200, 262144, 0),
-          ("f32", 3, 1000003, 5), ("bf16", 64, 150001, 20), ("bf16", 1, 32768, 5)]
+          ("f32", 3, 1000003, 5), ("bf16", 64, 150001, 20), ("bf16", 1, 32768, 5), ("bf16", 2048, 65537, 1), ("f16", 8192, 262143, 1),
+          ("f32", 2000, 24571, 3)]
 
 
 @pytest.mark.parametrize("name,rows,classes,top", SHAPES)
