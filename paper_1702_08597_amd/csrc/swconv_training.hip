@@ -180,13 +180,13 @@ int check_scores(int dtype, int64_t rows, int64_t classes, int64_t given, int64_
 }
 
 // How many waves share a row, and into how many parts it is cut.  A tile is what a wave reads at a time, 4 KB; aligned: every
-// row begins on 16 bytes.  Times of bf16 rows with entropies and the best class in us, inputs from memory:
+// row begins on 4 bytes.  Times of bf16 rows with entropies and the best class in us, inputs from memory:
 //   a wave per row where rows alone fill the chip, 7 to a CU (32768 classes of 1536 rows 35, four waves 31; of 1792 36 and 37,
 //   of 4096 64 and 74), for short rows, of which four waves get few tiles each, from 160 rows to a tile on (256 without best
 //   classes, whose second look costs four waves more), 4 to a CU at least (5): 16384 classes of 1024 rows 20 and 19, of 1280 22
 //   and 21, of 1536 22 and 23.  Up to 24 tiles: 49152 classes of 4096 rows 86 and 95, 131072 of them 228 and 221, fp32 24576
 //   classes 82 and 85, 65536 classes 222 and 208; up to 10 without best classes: 20480 classes of 4096 rows 37 and 41, 32768 60
-//   and 54.  16-bit rows that are not aligned, which four waves read more slowly (131035 classes of 4096 rows 231 and 263), at any
+//   and 54.  Rows that are not aligned, which four waves read more slowly (131035 classes of 4096 rows 231 and 263), at any
 //   length, with more than 8 best classes up to 32 tiles (2048 rows with the best 20: 65499 classes 80 and 81, 131035 classes
 //   158 and 144).  Rows of one or two tiles in any case;
 //   four waves of a workgroup, sixteen for rows of 12 tiles at least while a CU has only one of them: 131072 classes of 256
@@ -201,7 +201,7 @@ struct Parts {
 Parts parts_of(int dtype, int64_t rows, int64_t classes, int top, bool aligned) {
   const int64_t tile = 64 * (16 / size_of(dtype)) * kLogpUnroll, tiles = (classes + tile - 1) / tile;
   const int64_t filled = top ? std::clamp<int64_t>(160 * tiles, 1024, 1792) : std::clamp<int64_t>(256 * tiles, 1280, 1792);
-  const int64_t longest = aligned || dtype == SWCONV_F32 ? (top ? 24 : 10) : top > 8 ? 32 : tiles;
+  const int64_t longest = aligned ? (top ? 24 : 10) : top > 8 ? 32 : tiles;
   if (tiles <= 2 || (rows >= filled && tiles <= longest)) return {1, 1, classes};
   if (rows > 256 || tiles < 12) return {4, 1, classes};
   int64_t parts = 1;
@@ -346,7 +346,7 @@ int swconv_logprobs_forward(int dtype, int64_t rows, int64_t classes, const void
   for (const void* p : {(const void*)labels_dev, (const void*)logprob_dev, (const void*)entropy_dev, (const void*)stats_dev,
                         (const void*)top_class_dev, (const void*)top_logprob_dev})
     if ((uintptr_t)p % 4) return SWCONV_EINVAL;
-  const bool aligned = (uintptr_t)scores_dev % 16 == 0 && (rows == 1 || row_stride * size % 16 == 0);
+  const bool aligned = (uintptr_t)scores_dev % 4 == 0 && row_stride * size % 4 == 0;
   const Parts pt = parts_of(dtype, rows, classes, top, aligned);
   if (pt.parts > 1 &&
       (!workspace_dev || (uintptr_t)workspace_dev % 16 || workspace_bytes < parts_bytes(pt, rows, top)))
