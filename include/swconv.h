@@ -369,6 +369,7 @@ typedef enum {
  *               a layer would have the mask that the next one had a pass earlier), or has a state of its own for each layer.
  *   y_dev       DEVICE, N x K x S with y_stride; may be x_dev with the same stride, else shares no element with x.
  *               What lies between the images is not written, and what it holds does not matter.
+ * The outputs of this call and those below share no memory with any other argument but where it says so.
  * The mask is a function of the sizes and the four numbers alone, whatever dtype, strides and launch: with
  * row = n*K + k, col = s (S = 1: row = n, col = k) an element is kept if the 16-bit field col % 8 (low half of word 0
  * first) of philox4x32-10 at counter {col / 8, row, low and high word of step + offset} with the seed as key is not

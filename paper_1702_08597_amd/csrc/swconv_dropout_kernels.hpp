@@ -6,8 +6,8 @@
 // element's decision alone and the backward pass makes the forward pass's.  An item of 8 columns costs one call, 20
 // products of 32 x 32 bits.  16 bits an element round the rate to a multiple of 2^-16; the scale is that rate's, so the
 // mean is kept exactly.  Arithmetic in fp32, one rounding to the element type at the end.
-// Bound by memory: 32 x 256 x 56 x 56 fp32 5.0 TB/s read and written (41 us), 16384 x 4096 fp32 5.7, bf16 4.8 (56 us), where the
-// generator's products and the unpacking keep the vector units 67 % busy.
+// Bound by memory: 32 x 256 x 56 x 56 fp32 5.0 TB/s read and written (41 us), 16384 x 4096 fp32 5.6, bf16 5.0 (53 us), where the
+// generator's products and the unpacking keep the vector units 69 % busy.
 #pragma once
 #include "swconv_elements.hpp"
 #include "swconv_lanes.hpp"

@@ -10,10 +10,10 @@
 // share of a row).  The t-th largest of the lanes' largest scores is a bar that t scores reach and few others: the lanes and
 // segments that reach it are read again, a lane to a score, and what reaches it is sorted, as 64-bit keys (score, then
 // the lower class), one to a lane.  (Keeping the best up to date within the pass, 4096 x 131072 bf16 took 239 us for the best
-// one and 413 for 64; so it takes 207 and 242, without any 182.)
-// What bounds the forward pass: memory for many long rows - 4096 x 131072 bf16 with entropies at 5.9 TB/s, five vector
-// instructions and an exponential to a score, which is 80 % of what the vector units issue; the way through one wave's
-// tile, sorts and joins for few rows (1 x 32768 10 us, 256 x 1000 with the best 5 7 us, 4.5 without any).
+// one and 413 for 64; so it takes 191 and 241, without any 186.)
+// What bounds the forward pass: the vector units for many long rows - 4096 x 131072 bf16 with entropies and the best class at 5.6
+// TB/s, 10 vector instructions to a score, which keep them 95 % busy; the way through one wave's tile, sorts and joins for few
+// rows (1 x 32768 10 us, 256 x 1000 with the best 5 7 us, 4 without any).
 #pragma once
 #include "swconv_elements.hpp"
 #include "swconv_lanes.hpp"
@@ -526,7 +526,7 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(int64_t rows, int64_
 
 // ---- backward ---------------------------------------------------------------------------------------------------
 // With e = exp(x - m) and p = e exp(-ls):  d x = -p (g + h (x - m - ls + H)) = e (b + a log2 e), a and b by row.  The
-// exponent holds x - m alone: ls in it would cost the digits of its size.  Bound by memory: 4096 x 131072 bf16 at 6.1 TB/s
+// exponent holds x - m alone: ls in it would cost the digits of its size.  Bound by memory: 4096 x 131072 bf16 at 6.0 TB/s
 // read and written.
 struct GradRow {
   float m, a, b, g;
