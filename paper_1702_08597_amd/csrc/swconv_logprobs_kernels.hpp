@@ -531,7 +531,7 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(int64_t rows, int64_
 struct GradRow {
   float m, a, b, g;
   int32_t label;
-  bool plain;  // all of them are finite
+  bool plain;  // all of them are finite, and b + a log2 e for every exponential
 };
 struct GradIn {
   const int32_t* labels;
@@ -549,7 +549,7 @@ __device__ __forceinline__ GradRow grad_row(const GradIn& in, int64_t row, int64
   const float scale = -__builtin_amdgcn_exp2f(-u) * __builtin_fmaf(-low, kLn2, 1.0f);
   r.a = scale * h * kLn2;
   r.b = scale * (r.g + h * (H - ls));
-  r.plain = fabsf(r.m) < INFINITY && fabsf(r.a) < INFINITY && fabsf(r.b) < INFINITY;
+  r.plain = fabsf(r.m) < INFINITY && fabsf(r.a) < 1e35f && fabsf(r.b) < 1e38f;
   return r;
 }
 // 16 bytes of scores that begin with class j into 16 bytes of gradients.
@@ -574,11 +574,13 @@ __device__ __forceinline__ Words grad_words(const GradRow& r, const Words& x, in
           out.v[i] = (elem_t<E>)(xi > -INFINITY ? r.g + __builtin_amdgcn_exp2f(d) * __builtin_fmaf(r.a, d, r.b) : 0.0f);
         }
   } else {
-    // no class left (all 0), a row of NaN, or a gradient that is not finite; masked classes get 0 here too
+    // no class left (all 0), a row of NaN, or a gradient that is not finite or near the end of fp32, where an exponential of 0
+    // comes before any product; masked classes get 0 here too
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float xi = word_elem<E>(x, i), d = fmaxf((xi - r.m) * kLog2e, kFarBelow);
-      float v = r.m != r.m ? NAN : __builtin_amdgcn_exp2f(d) * (r.a * d + r.b);
+      const float e = __builtin_amdgcn_exp2f(d);
+      float v = r.m != r.m ? NAN : e * r.a * d + e * r.b;
       if (hot == i) v += r.g;
       out.v[i] = (elem_t<E>)(xi == -INFINITY ? 0.0f : v);
     }
